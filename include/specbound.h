@@ -444,6 +444,117 @@ int32_t sb_op_prompt_attention(const float *qkv, int32_t n_heads, int32_t n_kv_h
                                const int32_t *table, int32_t n_pages, int32_t layer, const float *rope_cos,
                                const float *rope_sin, int32_t pos0, int32_t M, float *out, void *stream);
 
+/* ---- a paged cache that many sequences live in ------------------------------ */
+/* The operators below work on the newest rows of several sequences of any lengths, whose keys and
+ * values lie in the pages of one bf16 pool (the layout sb_op_attention gives: [layer][2 (k, v)]
+ * [n_pages][n_kv_heads][SB_KV_BLOCK][head_dim], v slabs transposed).  Sequence b's newest rows are
+ * rows row_start[b] .. row_start[b + 1] - 1 of the operands; the last of them is at position
+ * kv_len[b] - 1.  table[b][i] is the page of its keys 16 i .. 16 i + 15.
+ *   What lies on the device is read when the kernels run (a captured call sees what stands there at
+ * each replay), so it cannot be refused.  It is bounded instead: row_start is cut to 0 .. n_rows,
+ * kv_len to 0 .. max_len; a page number outside 0 .. n_pages - 1 is never followed -- nothing is
+ * written for it, its keys and values read as zeros.  row_start has to ascend.  Rows of no sequence
+ * (before row_start[0], from row_start[n_seq] on) are neither read nor written. */
+typedef struct sb_paged {
+    void *pool;               /* device, 16-byte aligned */
+    const int32_t *table;     /* device [n_seq][table_ld]; only the entries of a sequence's kv_len keys are read */
+    const int32_t *row_start; /* device [n_seq + 1], ascending */
+    const int32_t *kv_len;    /* device [n_seq]: keys of each sequence, its newest rows among them */
+    int32_t n_pages, n_kv_heads, head_dim; /* head_dim 64 or 128 */
+    int32_t n_seq, n_rows;    /* sequences; rows of the operands (either may be 0: nothing is done) */
+    int32_t table_ld;         /* entries from one sequence's pages to the next's */
+    int32_t max_len;          /* no sequence is longer: 1 .. 16 table_ld */
+} sb_paged;
+
+enum { SB_ROPE_HALF = 0, SB_ROPE_INTERLEAVED = 1 };
+/* Rotary embedding and cache append of the newest rows.  qkv [n_rows][ld_qkv] in x_dtype (SB_FP32 or
+ * SB_BF16) holds each row's q heads, k heads and v heads.  Where q_gain / k_gain (device [head_dim],
+ * float) are given, a head x becomes x / sqrt(mean x^2 + eps) * gain first.  Its first rot_dim dims (a
+ * multiple of 8, 0 .. head_dim) are rotated by the row's position: pairs (i, i + rot_dim / 2), or
+ * (2 i, 2 i + 1) with SB_ROPE_INTERLEAVED, (a, b) -> (a c - b s, b c + a s) with c, s from rope_cos /
+ * rope_sin (device [n_pos][rot_dim / 2]; any table, see sb_rope_table_scaled_host).  Rotated q goes to
+ * q_out [n_rows][ld_q] in x_dtype, rotated k and v, rounded to bf16, to the pages of `layer`.  All in
+ * float, each output rounded once.  Two rows of a call must not be at one place of the pool.
+ * A row at a position outside 0 .. n_pos - 1 is neither read nor written (n_pos is not looked at with
+ * rot_dim 0); a position of max_len or more cannot arise.  q_out may be qkv itself (same ld), else it
+ * must not overlap it.  Operands 16-byte aligned, rows a multiple of 16 bytes apart. */
+int32_t sb_op_rope_append(const sb_paged *kv, int32_t layer, const void *qkv, int32_t x_dtype, int64_t ld_qkv, int32_t n_heads,
+                          const float *q_gain, const float *k_gain, float eps, const float *rope_cos, const float *rope_sin,
+                          int32_t n_pos, int32_t rot_dim, int32_t rope_layout, void *q_out, int64_t ld_q, void *stream);
+
+/* What a row at position p sees, and with which score.  A key at k of its sequence is seen if
+ *   k < kv_len, k >= doc_start[row], and  k < prefix_len  or  (k <= p and, with a window, k > p - window).
+ * Its score is s = scale q.k, then cap tanh(s / cap) with softcap = cap > 0, then less slopes[head] |p - k|.
+ * All zeros: plain causal attention. */
+typedef struct sb_attn_rule {
+    float scale;               /* 0: 1 / sqrt(head_dim); else > 0 */
+    float softcap;             /* 0: none; else > 0 */
+    const float *slopes;       /* NULL, or device [n_heads] */
+    int32_t window;            /* 0: none; else the row's own key counts: window 1 sees that alone */
+    const int32_t *prefix_len; /* NULL, or device [n_seq]: so many first keys are seen by every row (kv_len: all) */
+    const int32_t *doc_start;  /* NULL, or device [n_rows]: first position of the row's document */
+} sb_attn_rule;
+/* Attention of the newest rows over their sequences' pages (append them first: sb_op_rope_append).
+ * q [n_rows][ld_q] and out [n_rows][ld_out] in x_dtype; out may be q itself (same ld), else it must not
+ * overlap it; operands 16-byte aligned, rows a multiple of 16 bytes apart.  A row that sees no key gets
+ * zeros.  What is not seen does not matter, whatever bits it has; an infinity or NaN that is seen makes
+ * the outputs that it enters infinite or NaN.  SB_BF16: scores and sums are float, probabilities enter
+ * the product with V as bf16 (relative 2^-9 each, about what rounding the output costs).  SB_FP32: queries
+ * and probabilities are carried with all 24 bits.  rule NULL: plain causal.  scratch: device, 256-byte aligned,
+ * sb_op_paged_attention_scratch_bytes() bytes (SB_ENOMEM if fewer; needs no clearing; NULL where that is
+ * 0).  The order of additions depends on the sizes in `kv`, not on the rows beside a row. */
+int32_t sb_op_paged_attention(const sb_paged *kv, int32_t layer, const void *q, int32_t x_dtype, int64_t ld_q, int32_t n_heads,
+                              const sb_attn_rule *rule, void *out, int64_t ld_out, void *scratch, size_t scratch_bytes,
+                              void *stream);
+size_t sb_op_paged_attention_scratch_bytes(const sb_paged *kv, int32_t n_heads);
+
+/* Copies whole pages: page src_pages[i] of src to page dst_pages[i] of dst, in each of n_slabs slabs (2 per
+ * layer: [n_slabs][n_pages][page_bytes], page_bytes = n_kv_heads SB_KV_BLOCK head_dim elements, any cache
+ * type).  The page lists are host memory, read during the call.  Page numbers out of range, a page written
+ * twice, pools that overlap without being the same, and in one pool (src == dst, the same page count) a page
+ * that is both written and read are refused; a page may be read any number of times.  Pools 16-byte aligned, page_bytes a
+ * multiple of 16. */
+int32_t sb_op_copy_pages(void *dst, int32_t dst_n_pages, const void *src, int32_t src_n_pages, size_t page_bytes,
+                         int32_t n_slabs, const int32_t *dst_pages, const int32_t *src_pages, int32_t n, void *stream);
+
+/* sb_op_copy_pages between two sessions: dst continues where src stands (committed tokens, pending token,
+ * draft-step counter; statistics cleared), each with its own cache from then on.  One prompt pass serves
+ * several continuations.  The sessions are of one model; SB_ESTATE if src has open rows or no pending token.
+ * dst's earlier contents are dropped, as sb_prefill drops them. */
+int32_t sb_fork_session(sb_session *dst, sb_session *src);
+
+/* Who uses which page of a pool: host bookkeeping beside the operators above, no device memory.  A page is
+ * free or has a count of users.  Calls on one sb_pages must not overlap.  A call that fails changes nothing. */
+typedef struct sb_pages sb_pages;
+int32_t sb_new_pages(int32_t n_pages, sb_pages **out);
+void sb_free_pages(sb_pages *p);
+/* n free pages, lowest numbers first, with one user each.  SB_ECAPACITY if there are fewer. */
+int32_t sb_pages_alloc(sb_pages *p, int32_t n, int32_t *out);
+/* One more user for each page of the list (a page listed twice gets two); SB_EINVAL if one is free. */
+int32_t sb_pages_share(sb_pages *p, const int32_t *pages, int32_t n);
+/* One user less for each; pages without users are free again.  SB_EINVAL if a page has fewer users than
+ * the list names it. */
+int32_t sb_pages_release(sb_pages *p, const int32_t *pages, int32_t n);
+/* Users of a page (0: free), or SB_EINVAL.  sb_pages_used: pages that have users. */
+int32_t sb_pages_users(const sb_pages *p, int32_t page);
+int32_t sb_pages_used(const sb_pages *p);
+/* Closes the holes: every used page at or above the number of used pages moves to a free one below it.
+ * src[i] -> dst[i], i < *n_moves, for sb_op_copy_pages and the caller's tables; users move with the page.
+ * SB_ECAPACITY, with *n_moves the number needed, if cap is too small. */
+int32_t sb_pages_compact(sb_pages *p, int32_t *src, int32_t *dst, int32_t cap, int32_t *n_moves);
+
+/* Rotary tables for contexts beyond the trained one: cos/sin of pos * f_i, [n_pos][rot_dim / 2] each, host,
+ * evaluated in double and rounded to float, times `magnitude` (1: none).  f_i = base^(-2 i / rot_dim), and
+ *   SB_ROPE_PLAIN   as it is (sb_rope_table_host);
+ *   SB_ROPE_LINEAR  f_i / factor (positions squeezed into the trained range);
+ *   SB_ROPE_BASE    base * factor^(rot_dim / (rot_dim - 2)): the slowest frequency is divided by factor, the fastest kept;
+ *   SB_ROPE_PARTS   by the turns r_i = orig_len f_i / (2 pi) within the trained length: f_i / factor up to `slow`
+ *                   turns, f_i from `fast` turns on, in between (1 - t) f_i / factor + t f_i, t = (r_i - slow) / (fast - slow).
+ * factor >= 1; orig_len >= 1 and 0 <= slow < fast for SB_ROPE_PARTS, else not looked at. */
+enum { SB_ROPE_PLAIN = 0, SB_ROPE_LINEAR = 1, SB_ROPE_BASE = 2, SB_ROPE_PARTS = 3 };
+int32_t sb_rope_table_scaled_host(int32_t rot_dim, float base, int32_t n_pos, int32_t kind, float factor, int32_t orig_len,
+                                  float slow, float fast, float magnitude, float *cos_out, float *sin_out);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,6 +19,8 @@ OK, EINVAL, ENOMEM, ECAPACITY, ESTATE, EDEVICE = 0, -1, -2, -3, -4, -5
 FP32, BF16 = 0, 1
 EXITED, WIDTH_BOUND, DEPTH_BOUND = 1, 2, 3
 PROJ_AUTO, PROJ_VALU, PROJ_MFMA, PROJ_MFMA_PACKED = 0, 1, 2, 3
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
 
 
 class SbError(RuntimeError):
@@ -80,6 +82,16 @@ class sb_sizes(C.Structure):
                 ("packed_weight_bytes", C.c_size_t)]
 
 
+class sb_paged(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("pool", "table", "row_start", "kv_len")] + \
+               [(n, C.c_int32) for n in ("n_pages", "n_kv_heads", "head_dim", "n_seq", "n_rows", "table_ld", "max_len")]
+
+
+class sb_attn_rule(C.Structure):
+    _fields_ = [("scale", C.c_float), ("softcap", C.c_float), ("slopes", C.c_void_p), ("window", C.c_int32),
+                ("prefix_len", C.c_void_p), ("doc_start", C.c_void_p)]
+
+
 # every symbol include/specbound.h declares
 SYMBOLS = ["sb_last_error", "sb_temperature_schedule", "sb_query_sizes", "sb_load_model", "sb_free_model",
            "sb_new_session", "sb_free_session", "sb_prefill", "sb_draft_step", "sb_verify", "sb_generate",
@@ -88,7 +100,9 @@ SYMBOLS = ["sb_last_error", "sb_temperature_schedule", "sb_query_sizes", "sb_loa
            "sb_op_head_scratch_bytes", "sb_rope_table_host", "sb_op_attention",
            "sb_op_attention_scratch_bytes", "sb_op_prompt_attention", "sb_decode", "sb_rewind", "sb_profile_begin", "sb_profile_end", "sb_op_copy",
            "sb_op_read", "sb_op_repack", "sb_op_gemm", "sb_op_gemm_scratch_bytes", "sb_op_head_static", "sb_phase_timing", "sb_debug_fail_launch", "sb_open_rows", "sb_new_batch", "sb_free_batch",
-           "sb_batch_decode"]
+           "sb_batch_decode", "sb_op_rope_append", "sb_op_paged_attention", "sb_op_paged_attention_scratch_bytes",
+           "sb_op_copy_pages", "sb_fork_session", "sb_new_pages", "sb_free_pages", "sb_pages_alloc", "sb_pages_share",
+           "sb_pages_release", "sb_pages_users", "sb_pages_used", "sb_pages_compact", "sb_rope_table_scaled_host"]
 
 KERNEL_CLASSES = ["rmsnorm", "qkv", "attention", "wo", "gate_up", "down", "exit_head",
                   "final_head"]
@@ -157,6 +171,23 @@ def lib() -> C.CDLL:
         L.sb_op_attention_scratch_bytes.argtypes = [i32, i32, i32, i32]
         L.sb_op_prompt_attention.argtypes = [vp, i32, i32, i32, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp]
         L.sb_op_attention_scratch_bytes.restype = sz
+        i64, kvp = C.c_int64, C.POINTER(sb_paged)
+        L.sb_op_rope_append.argtypes = [kvp, i32, vp, i32, i64, i32, vp, vp, f32, vp, vp, i32, i32, i32, vp, i64, vp]
+        L.sb_op_paged_attention.argtypes = [kvp, i32, vp, i32, i64, i32, C.POINTER(sb_attn_rule), vp, i64, vp, sz, vp]
+        L.sb_op_paged_attention_scratch_bytes.argtypes = [kvp, i32]
+        L.sb_op_paged_attention_scratch_bytes.restype = sz
+        L.sb_op_copy_pages.argtypes = [vp, i32, vp, i32, sz, i32, vp, vp, i32, vp]
+        L.sb_fork_session.argtypes = [vp, vp]
+        L.sb_new_pages.argtypes = [i32, C.POINTER(vp)]
+        L.sb_free_pages.argtypes = [vp]
+        L.sb_free_pages.restype = None
+        L.sb_pages_alloc.argtypes = [vp, i32, vp]
+        L.sb_pages_share.argtypes = [vp, vp, i32]
+        L.sb_pages_release.argtypes = [vp, vp, i32]
+        L.sb_pages_users.argtypes = [vp, i32]
+        L.sb_pages_used.argtypes = [vp]
+        L.sb_pages_compact.argtypes = [vp, vp, vp, i32, C.POINTER(i32)]
+        L.sb_rope_table_scaled_host.argtypes = [i32, f32, i32, i32, f32, i32, f32, f32, f32, vp, vp]
         _lib = L
     return _lib
 
@@ -363,6 +394,16 @@ class Session:
 
     def rewind(self, n_keep: int, pending_token: int, draft_counter: int = 0):
         check(lib().sb_rewind(self.h, n_keep, int(pending_token), draft_counter))
+
+    def fork(self, page_order: Optional[Sequence[int]] = None) -> "Session":
+        """A new session that continues where this one stands, on a cache of its own (sb_fork_session)."""
+        s = Session(self.model, page_order)
+        s.fork_from(self)
+        return s
+
+    def fork_from(self, src: "Session"):
+        """Drop what this session holds and continue where `src` stands."""
+        check(lib().sb_fork_session(self.h, src.h))
 
     def profile_begin(self, classes=None, max_launches: int = 1 << 16, sample_every: int = 1):
         mask = 0
@@ -609,3 +650,237 @@ def op_read(src, sink):
     import torch
     check(lib().sb_op_read(src.data_ptr(), src.numel() * src.element_size(), sink.data_ptr(),
                            _stream_ptr(torch, src)))
+
+
+# ------------------------------------------------- a paged cache of several sequences
+def _dtype_code(t):
+    import torch
+    if t.dtype == torch.float32:
+        return FP32
+    if t.dtype == torch.bfloat16:
+        return BF16
+    raise TypeError(f"expected float32 or bfloat16 rows, not {t.dtype}")
+
+
+def _need(t, name, device, dtype=None, ndim=None):
+    """A tensor argument on the GPU of the pool; its pointer (None stays None)."""
+    if t is None:
+        return None
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the pool on {device}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if ndim is not None and (t.dim() != ndim or not t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous with {ndim} dimension(s), not {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _rows(t, name, n_rows, width, device):
+    """Rows of a 2-d operand: its pointer, the elements from one row to the next."""
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the pool on {device}")
+    if t.dim() != 2 or t.shape[0] != n_rows or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [{n_rows}, {width}] with rows of neighbouring elements, not {tuple(t.shape)} of strides {t.stride()}")
+    return t.data_ptr(), t.stride(0) if n_rows > 1 else width
+
+
+class Paged:
+    """The newest rows of several sequences and the pages of one bf16 pool that they live in (sb_paged).
+
+    pool [n_layers, 2, n_pages, n_kv_heads, SB_KV_BLOCK, head_dim] bfloat16, contiguous (the values of a page lie
+    transposed in it, [head_dim][SB_KV_BLOCK]); table [n_seq, pages] int32; row_start [n_seq + 1] and kv_len [n_seq]
+    int32: sequence b's newest rows are rows row_start[b] .. row_start[b + 1] - 1 of the operands, the last of them at
+    position kv_len[b] - 1.  n_rows: rows of the operands.  max_len: no sequence is longer (default: what the table
+    holds).  All on one GPU; they may be changed in place between calls."""
+
+    def __init__(self, pool, table, row_start, kv_len, n_rows: int, max_len: Optional[int] = None):
+        import torch
+        if pool.dim() != 6 or pool.shape[1] != 2 or pool.shape[4] != SB_KV_BLOCK or not pool.is_contiguous():
+            raise ValueError(f"pool must be contiguous [n_layers, 2, n_pages, n_kv_heads, {SB_KV_BLOCK}, head_dim], not {tuple(pool.shape)}")
+        if pool.dtype != torch.bfloat16:
+            raise TypeError(f"pool must be bfloat16, not {pool.dtype}")
+        if not pool.is_cuda:
+            raise ValueError(f"expected a pool on a GPU, not on {pool.device}")
+        dev = pool.device
+        if table.dim() != 2 or table.shape[1] < 1 or (table.shape[1] > 1 and table.stride(1) != 1) or (table.shape[0] > 1 and table.stride(0) < table.shape[1]):
+            raise ValueError(f"table must be [n_seq, pages] with neighbouring pages, not {tuple(table.shape)} of strides {table.stride()}")
+        n_seq = table.shape[0]
+        if table.dtype != torch.int32:
+            raise TypeError(f"table must be torch.int32, not {table.dtype}")
+        if table.device != dev:
+            raise ValueError(f"table is on {table.device}, the pool on {dev}")
+        _need(row_start, "row_start", dev, torch.int32, 1)
+        _need(kv_len, "kv_len", dev, torch.int32, 1)
+        if row_start.shape[0] != n_seq + 1 or kv_len.shape[0] != n_seq:
+            raise ValueError(f"{n_seq} sequences need row_start [{n_seq + 1}] and kv_len [{n_seq}], not {tuple(row_start.shape)} and {tuple(kv_len.shape)}")
+        cap = SB_KV_BLOCK * table.shape[1]
+        max_len = cap if max_len is None else int(max_len)
+        if not 1 <= max_len <= cap:
+            raise ValueError(f"max_len must be in 1..{cap}, not {max_len}")
+        self.pool, self.table, self.row_start, self.kv_len = pool, table, row_start, kv_len
+        self.device, self.n_rows = dev, int(n_rows)
+        self.n_layers, _, self.n_pages, self.n_kv_heads, _, self.head_dim = pool.shape
+        ld = table.stride(0) if n_seq > 1 else table.shape[1]
+        self.c = sb_paged(pool.data_ptr(), table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(), self.n_pages, self.n_kv_heads,
+                          self.head_dim, n_seq, self.n_rows, ld, max_len)
+
+    def _call(self, layer, fn, *args):
+        import torch
+        if not 0 <= layer < self.n_layers:
+            raise ValueError(f"layer must be in 0..{self.n_layers - 1}, not {layer}")
+        st = torch._C._cuda_getCurrentRawStream(self.device.index)
+        if torch.cuda.current_device() == self.device.index:
+            return check(fn(C.byref(self.c), layer, *args, st))
+        with torch.cuda.device(self.device):
+            check(fn(C.byref(self.c), layer, *args, st))
+
+
+def op_rope_append(kv: Paged, qkv, n_heads: int, rope_cos, rope_sin, interleaved: bool = False, q_gain=None, k_gain=None,
+                   eps: float = 1e-6, out=None, layer: int = 0):
+    """Norm (where gains are given) and rotation of the q and k heads of kv's newest rows, k and v rounded into their
+    pages; returns the rotated q [n_rows, n_heads * head_dim] in qkv's type.
+
+    qkv [n_rows, (n_heads + 2 n_kv_heads) head_dim] float32 or bfloat16; rope_cos, rope_sin [n_pos, rot_dim / 2] float32
+    (rot_dim dims of a head are rotated, the others passed); gains [head_dim] float32.  `out` may be a tensor for the
+    result, or the first n_heads * head_dim columns of qkv themselves."""
+    import torch
+    hd, dev = kv.head_dim, kv.device
+    w = n_heads * hd
+    x, ld = _rows(qkv, "qkv", kv.n_rows, (n_heads + 2 * kv.n_kv_heads) * hd, dev)
+    code = _dtype_code(qkv)
+    if rope_cos.shape != rope_sin.shape:
+        raise ValueError(f"rope tables of {tuple(rope_cos.shape)} and {tuple(rope_sin.shape)}")
+    cp, sp = _need(rope_cos, "rope_cos", dev, torch.float32, 2), _need(rope_sin, "rope_sin", dev, torch.float32, 2)
+    qg, kg = _need(q_gain, "q_gain", dev, torch.float32, 1), _need(k_gain, "k_gain", dev, torch.float32, 1)
+    for g in (q_gain, k_gain):
+        if g is not None and g.shape[0] != hd:
+            raise ValueError(f"a gain of {g.shape[0]} for heads of {hd}")
+    if out is None:
+        out = torch.empty((kv.n_rows, w), dtype=qkv.dtype, device=dev)
+    elif out.dtype != qkv.dtype:
+        raise TypeError(f"out must be {qkv.dtype}, not {out.dtype}")
+    o, ldo = _rows(out, "out", kv.n_rows, w, dev)
+    if kv.n_rows == 1 and o == x:
+        ldo = ld
+    kv._call(layer, lib().sb_op_rope_append, x, code, ld, n_heads, qg, kg, eps, cp, sp, rope_cos.shape[0], 2 * rope_cos.shape[1],
+             ROPE_INTERLEAVED if interleaved else ROPE_HALF, o, ldo)
+    return out
+
+
+def paged_attention_scratch(kv: Paged, n_heads: int):
+    """A scratch area for op_paged_attention calls on kv (calls that may overlap need one each)."""
+    import torch
+    n = lib().sb_op_paged_attention_scratch_bytes(C.byref(kv.c), n_heads)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=kv.device)
+
+
+def op_paged_attention(kv: Paged, q, n_heads: int, scale: float = 0.0, softcap: float = 0.0, slopes=None, window: int = 0,
+                       prefix_len=None, doc_start=None, out=None, scratch=None, layer: int = 0):
+    """Attention of kv's newest rows over their sequences' pages; returns [n_rows, n_heads * head_dim] in q's type
+    (float32 or bfloat16).  `out` may be a tensor for the result, also q itself.
+
+    A row at position p sees key k of its sequence if k >= doc_start[row] and (k < prefix_len[sequence], or k <= p and, with
+    a window, k > p - window).  Scores: scale q.k (0: 1 / sqrt(head_dim)), softcap * tanh(. / softcap) where softcap > 0,
+    less slopes[head] * |p - k|.  slopes [n_heads] float32, prefix_len [n_seq] and doc_start [n_rows] int32."""
+    import torch
+    dev = kv.device
+    w = n_heads * kv.head_dim
+    x, ld = _rows(q, "q", kv.n_rows, w, dev)
+    code = _dtype_code(q)
+    rule = sb_attn_rule(scale, softcap, _need(slopes, "slopes", dev, torch.float32, 1), window,
+                        _need(prefix_len, "prefix_len", dev, torch.int32, 1), _need(doc_start, "doc_start", dev, torch.int32, 1))
+    for t, name, n in ((slopes, "slopes", n_heads), (prefix_len, "prefix_len", kv.c.n_seq), (doc_start, "doc_start", kv.n_rows)):
+        if t is not None and t.shape[0] != n:
+            raise ValueError(f"{name} must have {n} entries, not {t.shape[0]}")
+    if out is None:
+        out = torch.empty((kv.n_rows, w), dtype=q.dtype, device=dev)
+    elif out.dtype != q.dtype:
+        raise TypeError(f"out must be {q.dtype}, not {out.dtype}")
+    o, ldo = _rows(out, "out", kv.n_rows, w, dev)
+    if kv.n_rows == 1 and o == x:
+        ldo = ld
+    if scratch is None:
+        scratch = paged_attention_scratch(kv, n_heads)
+    elif scratch.device != dev or not scratch.is_contiguous():
+        raise ValueError(f"scratch must be contiguous on {dev}")
+    kv._call(layer, lib().sb_op_paged_attention, x, code, ld, n_heads, C.byref(rule), o, ldo, scratch.data_ptr(),
+             scratch.numel() * scratch.element_size())
+    return out
+
+
+def op_copy_pages(dst, src, dst_pages: Sequence[int], src_pages: Sequence[int]):
+    """Page src_pages[i] of src -> page dst_pages[i] of dst, keys and values of all layers.  Pools [n_layers, 2, n_pages,
+    n_kv_heads, SB_KV_BLOCK, head_dim] of any cache type, alike but for n_pages; dst may be src."""
+    import torch
+    for t, name in ((dst, "dst"), (src, "src")):
+        if t.dim() != 6 or t.shape[1] != 2 or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError(f"{name} must be a contiguous pool [n_layers, 2, n_pages, n_kv_heads, {SB_KV_BLOCK}, head_dim] on a GPU")
+    if dst.shape[:2] != src.shape[:2] or dst.shape[3:] != src.shape[3:] or dst.dtype != src.dtype or dst.device != src.device:
+        raise ValueError(f"pools differ: {tuple(dst.shape)} {dst.dtype} {dst.device}, {tuple(src.shape)} {src.dtype} {src.device}")
+    d, s = (np.ascontiguousarray(p, dtype=np.int32) for p in (dst_pages, src_pages))
+    if d.ndim != 1 or d.shape != s.shape:
+        raise ValueError("dst_pages and src_pages must be lists of one length")
+    page_bytes = src[0, 0, 0].numel() * src.element_size()
+    with torch.cuda.device(src.device):
+        check(lib().sb_op_copy_pages(dst.data_ptr(), dst.shape[2], src.data_ptr(), src.shape[2], page_bytes, 2 * src.shape[0], d.ctypes.data,
+                                     s.ctypes.data, len(d), _stream_ptr(torch, src)))
+
+
+class Pages:
+    """Who uses which page of a pool (sb_pages): host bookkeeping, no device memory."""
+
+    def __init__(self, n_pages: int):
+        self.h = C.c_void_p()
+        check(lib().sb_new_pages(n_pages, C.byref(self.h)))
+        self.n_pages = n_pages
+
+    def alloc(self, n: int) -> np.ndarray:
+        """n free pages, lowest numbers first."""
+        out = np.empty(max(n, 0), dtype=np.int32)
+        check(lib().sb_pages_alloc(self.h, n, out.ctypes.data))
+        return out
+
+    def share(self, pages):
+        """One more user for each page (a sequence forked without copying its full pages)."""
+        p = np.ascontiguousarray(pages, dtype=np.int32)
+        check(lib().sb_pages_share(self.h, p.ctypes.data, p.size))
+
+    def release(self, pages):
+        p = np.ascontiguousarray(pages, dtype=np.int32)
+        check(lib().sb_pages_release(self.h, p.ctypes.data, p.size))
+
+    def users(self, page: int) -> int:
+        n = lib().sb_pages_users(self.h, page)
+        if n < 0:
+            check(n)
+        return n
+
+    def used(self) -> int:
+        return lib().sb_pages_used(self.h)
+
+    def compact(self):
+        """(src, dst): the moves that bring all used pages below used(), for op_copy_pages and the tables."""
+        src, dst = np.empty(self.n_pages, dtype=np.int32), np.empty(self.n_pages, dtype=np.int32)
+        n = C.c_int32()
+        check(lib().sb_pages_compact(self.h, src.ctypes.data, dst.ctypes.data, self.n_pages, C.byref(n)))
+        return src[:n.value].copy(), dst[:n.value].copy()
+
+    def close(self):
+        if self.h:
+            lib().sb_free_pages(self.h)
+            self.h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def rope_table_scaled(rot_dim: int, base: float, n_pos: int, kind: int = ROPE_PLAIN, factor: float = 1.0, orig_len: int = 0,
+                      slow: float = 1.0, fast: float = 32.0, magnitude: float = 1.0):
+    """(cos, sin) [n_pos, rot_dim / 2] float32 (numpy) for contexts `factor` times the trained length (sb_rope_table_scaled_host)."""
+    c = np.empty((n_pos, rot_dim // 2), dtype=np.float32)
+    s = np.empty_like(c)
+    check(lib().sb_rope_table_scaled_host(rot_dim, base, n_pos, kind, factor, orig_len, slow, fast, magnitude, c.ctypes.data, s.ctypes.data))
+    return c, s

@@ -57,6 +57,7 @@ struct sb_session {
     char* ws;
     sbhost::WsLayout L;
     sb::KvLayout kv;
+    std::vector<int32_t> page_order;   // host copy of kv.table
     sb::DevRound* d_round;
     sb::DevRound* h_round;  // pinned host copy
     // Exit decisions that gate the host's next launch (computed exits) arrive without a copy: the

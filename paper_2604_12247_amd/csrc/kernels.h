@@ -266,6 +266,48 @@ hipError_t launch_prefill_embed(const void* E, int32_t w_dtype, int32_t vocab, i
 // x [M][K] float -> bf16 planes [2][plane_rows][K]
 hipError_t launch_prefill_split(const float* x, uint16_t* xs, int32_t plane_rows, int32_t M, int32_t K, hipStream_t st);
 
+// ---- a paged cache of several sequences (paged.hip) ----
+struct PagedKv {
+    uint16_t *k, *v;                 // the layer's slabs: [n_pages][n_kv_heads][SB_KV_BLOCK][head_dim], v transposed
+    const int32_t *table, *row_start, *kv_len;
+    int32_t n_pages, n_kv_heads, head_dim, n_seq, n_rows, table_ld, max_len;
+};
+struct RopeAppendArgs {
+    PagedKv kv;
+    const void* qkv;
+    void* q_out;
+    int64_t ld_qkv, ld_q;
+    const float *q_gain, *k_gain, *cos, *sin;
+    float eps;
+    int32_t x_dtype, n_heads, n_pos, rot_dim, interleaved;
+};
+hipError_t launch_rope_append(const RopeAppendArgs& a, hipStream_t st);
+
+struct PagedAttnArgs {
+    PagedKv kv;
+    const void* q;
+    void* out;
+    int64_t ld_q, ld_out;
+    int32_t x_dtype, n_heads, group;
+    float scale, cap;
+    const float* slopes;
+    int32_t window;
+    const int32_t *prefix_len, *doc_start;
+    float* scratch;
+};
+size_t paged_attention_scratch(const PagedKv& kv, int32_t n_heads);
+hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t st);
+
+// Pages named in the arguments of one launch (4 KB of arguments at most).
+#define SB_COPY_PAGES 448
+struct CopyPagesArgs {
+    const char* src;
+    char* dst;
+    size_t src_slab, dst_slab, page_bytes;   // bytes
+    int32_t from[SB_COPY_PAGES], to[SB_COPY_PAGES];
+};
+hipError_t launch_copy_pages(const CopyPagesArgs& a, int32_t n, int32_t n_slabs, hipStream_t st);
+
 // Device memory that belongs to the library itself (a file-scope device array, one copy per
 // GPU): *out receives its address on the current device.  No allocation takes place.
 #define SB_STATIC_SCRATCH_BYTES (256 + SB_MAX_W * (SB_STATIC_MAX_N / 16) * 16)

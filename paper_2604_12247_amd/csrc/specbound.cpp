@@ -976,6 +976,7 @@ int32_t sb_new_session(sb_model* m, void* kv_pool, size_t kv_bytes, void* worksp
     s->d_round = wsp<DevRound>(s, L.round);
     s->kv.pool = kv_pool; s->kv.table = wsp<int32_t>(s, L.table); s->kv.n_pages = L.n_pages;
     s->kv.n_kv_heads = m->cfg.n_kv_heads; s->kv.head_dim = m->cfg.head_dim; s->kv.kv_dtype = m->cfg.kv_dtype;
+    s->page_order.swap(table);
     s->debug = false;
     s->prof_mask = 0;
     s->prof_used = 0;
@@ -999,7 +1000,7 @@ int32_t sb_new_session(sb_model* m, void* kv_pool, size_t kv_bytes, void* worksp
         e = hipEventCreateWithFlags(&s->ev_main[i], hipEventDisableTiming);
         if (e == hipSuccess) e = hipEventCreateWithFlags(&s->ev_head[i], hipEventDisableTiming);
     }
-    if (e == hipSuccess) e = hipMemcpyAsync(wsp<int32_t>(s, L.table), table.data(), (size_t)L.n_pages * 4, hipMemcpyHostToDevice, m->stream);
+    if (e == hipSuccess) e = hipMemcpyAsync(wsp<int32_t>(s, L.table), s->page_order.data(), (size_t)L.n_pages * 4, hipMemcpyHostToDevice, m->stream);
     if (e == hipSuccess) e = launch_fill_u32(reinterpret_cast<uint32_t*>(s->d_round), sizeof(DevRound) / 4, 0u, m->stream);
     if (e == hipSuccess) e = hipStreamSynchronize(m->stream);
     if (e != hipSuccess) {
@@ -1085,6 +1086,28 @@ int32_t sb_rewind(sb_session* s, int32_t n_keep, int32_t pending_token, int64_t 
     s->pending = pending_token;
     s->has_pending = true;
     s->draft_counter = draft_counter;
+    return SB_OK;
+}
+
+int32_t sb_fork_session(sb_session* dst, sb_session* src) {
+    if (!dst || !src) return fail(SB_EINVAL, "fork_session: session is NULL");
+    if (dst == src) return fail(SB_EINVAL, "fork_session: a session cannot be forked into itself");
+    if (dst->m != src->m) return fail(SB_EINVAL, "fork_session: the sessions are of different models");
+    if (src->n_slots) return fail(SB_ESTATE, "fork_session: a round of the source is open, call sb_verify first");
+    if (!src->has_pending) return fail(SB_ESTATE, "fork_session: no pending token (prefill first)");
+    const sb_config& c = src->m->cfg;
+    const int n = (src->c + SB_KV_BLOCK - 1) / SB_KV_BLOCK;
+    HIP_TRY(sync_all(dst));   // (its heads of an abandoned round may still be running on its own stream)
+    const size_t page_bytes = (size_t)c.n_kv_heads * SB_KV_BLOCK * c.head_dim * esize(c.kv_dtype);
+    const int rc = sb_op_copy_pages(dst->kv.pool, dst->kv.n_pages, src->kv.pool, src->kv.n_pages, page_bytes, 2 * c.n_layers, dst->page_order.data(),
+                                    src->page_order.data(), n, src->m->stream);
+    if (rc && rc != SB_EDEVICE) return rc;
+    reset_session(dst);   // (after a failed copy too: its cache may hold some of the pages)
+    if (rc) return rc;
+    dst->c = src->c;
+    dst->pending = src->pending;
+    dst->has_pending = true;
+    dst->draft_counter = src->draft_counter;
     return SB_OK;
 }
 
