@@ -2,6 +2,8 @@
 #include "kernels.h"
 #include "device_utils.h"
 
+#include <type_traits>
+
 namespace sb {
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
@@ -115,55 +117,546 @@ __device__ __forceinline__ Sees row_sees(const PagedAttnArgs& a, const SeqRows& 
     return v;
 }
 
-// A wave per row and head: 64 keys at a time, a lane each, with a running maximum and sum; then a lane holds HD / 64 dims.
-template <int HD>
-__global__ __launch_bounds__(64) void paged_attn_kernel(PagedAttnArgs a) {
-    __shared__ float qs[HD];
-    const int lane = threadIdx.x, row = blockIdx.x, head = blockIdx.y, Hkv = a.kv.n_kv_heads, g = head / a.group;
-    const SeqRows s = seq_rows(a.kv, find_seq(a.kv.n_seq, [&](int b) { return row_at(a.kv, b); }, row));
-    if (s.b < 0 || row >= s.r0 + s.n) return;
-    const int pos = s.len - s.n + row - s.r0;
-    const bool fp32 = a.x_dtype == SB_FP32;
-    for (int d = lane; d < HD; d += 64) qs[d] = load_x(a.q, (int64_t)row * a.ld_q + head * HD + d, fp32);
-    __syncthreads();
-    const Sees see = row_sees(a, s, row, pos);
-    float m = -SB_INF, l = 0.f, o[HD / 64] = {};
-    for (int k0 = 0; k0 < s.len; k0 += 64) {
-        const int key = k0 + lane;
-        float sc = -SB_INF;
-        if ((key >= see.a0 && key < see.a1) || (key >= see.b0 && key < see.b1)) {
-            const int pg = a.kv.table[(int64_t)s.b * a.kv.table_ld + key / SB_KV_BLOCK];
-            float z = 0.f;
-            if (pg >= 0 && pg < a.kv.n_pages) {
-                const uint16_t* kp = a.kv.k + (((int64_t)pg * Hkv + g) * SB_KV_BLOCK + key % SB_KV_BLOCK) * HD;
-                for (int d = 0; d < HD; ++d) z = fmaf(qs[d], bf2f(kp[d]), z);
-            }
-            sc = z * a.scale;
-            if (a.cap > 0.f) sc = a.cap * tanhf(sc / a.cap);
-            if (a.slopes) sc -= a.slopes[head] * fabsf((float)(pos - key));
-        }
-        const float m1 = fmaxf(m, wave_max(sc)), ref = m1 == -SB_INF ? 0.f : m1;
-        const float p = expf(sc - ref), f = expf((m == -SB_INF ? ref : m) - ref);
-        l = l * f + wave_sum(p);
-        for (int i = 0; i < HD / 64; ++i) o[i] *= f;
-        m = m1;
-        for (int j = 0; j < 64 && k0 + j < s.len; ++j) {
-            const float pj = __shfl(p, j, 64), sj = __shfl(sc, j, 64);
-            if (sj == -SB_INF) continue;
-            const int kj = k0 + j, pg = a.kv.table[(int64_t)s.b * a.kv.table_ld + kj / SB_KV_BLOCK];
-            if (pg < 0 || pg >= a.kv.n_pages) continue;
-            const uint16_t* vp = a.kv.v + ((int64_t)pg * Hkv + g) * SB_KV_BLOCK * HD + kj % SB_KV_BLOCK;
-            for (int i = 0; i < HD / 64; ++i) o[i] = fmaf(pj, bf2f(vp[(i * 64 + lane) * SB_KV_BLOCK]), o[i]);
-        }
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef uint16_t u16x2v __attribute__((ext_vector_type(2)));
+constexpr float LOG2E = 1.4426950408889634f;
+
+// least / largest over the 32 lanes of a half wave
+template <int O = 16>
+__device__ __forceinline__ int half_min(int v) {
+    uint32_t x, y;
+    lane_pair<O>((uint32_t)v, x, y);
+    const int m = (int)x < (int)y ? (int)x : (int)y;
+    if constexpr (O > 1) return half_min<O / 2>(m);
+    else return __builtin_amdgcn_readfirstlane(m);
+}
+__device__ __forceinline__ int half_max(int v) { return -half_min(-v); }
+
+// Query tiles of TQ (row, head of the group) pairs each, by sequence: sequence b's tiles start at row_start[b] G / TQ + b, which
+// leaves each at least as many as it needs whatever the row counts are (a tile past them has no query).
+template <int TQ>
+__device__ __forceinline__ SeqRows tile_seq(const PagedAttnArgs& a, int t, int& q0) {
+    const int G = a.group;
+    const auto first = [&](int b) { return row_at(a.kv, b) * G / TQ + b; };
+    const int b = __builtin_amdgcn_readfirstlane(find_seq(a.kv.n_seq, first, t));
+    SeqRows s = seq_rows(a.kv, b);
+    q0 = 0;
+    if (s.b >= 0) {
+        q0 = (t - (s.r0 * G / TQ + b)) * TQ;
+        if (q0 >= s.n * G) s.b = -1;
     }
-    for (int i = 0; i < HD / 64; ++i) store_x(a.out, (int64_t)row * a.ld_out + head * HD + i * 64 + lane, fp32, l == 0.f ? 0.f : o[i] / l);
+    return s;
 }
 
-size_t paged_attention_scratch(const PagedKv&, int32_t) { return 0; }
+// A lane's query: where it is, and the keys that it sees as two ranges [a0, a0 + an), [b0, b0 + bn).
+struct Query {
+    int row, head, pos, a0, b0;
+    uint32_t an, bn;
+    bool valid;
+    float slope2;   // in units of log 2
+};
+// What all 32 queries of a wave see (whole ranges), and bounds of what any of them does; scalars.
+struct Reach { int a_lo, a_hi, b_lo, b_hi, a0_max, a1_min, b0_max, b1_min; };
+
+__device__ __forceinline__ Query lane_query(const PagedAttnArgs& a, const SeqRows& s, int g, int qq, Reach& w) {
+    Query q;
+    const int G = a.group, r = qq / G;
+    q.valid = qq < s.n * G;
+    q.row = s.r0 + (q.valid ? r : 0);
+    q.head = g * G + (q.valid ? qq - r * G : 0);
+    q.pos = s.len - s.n + q.row - s.r0;
+    const Sees v = row_sees(a, s, q.row, q.pos);
+    q.a0 = v.a0; q.b0 = v.b0;
+    q.an = q.valid && v.a1 > v.a0 ? v.a1 - v.a0 : 0;
+    q.bn = q.valid && v.b1 > v.b0 ? v.b1 - v.b0 : 0;
+    q.slope2 = a.slopes ? a.slopes[q.head] * LOG2E : 0.f;
+    const int big = 0x7fffffff;
+    w.a_lo = half_min(q.an ? v.a0 : big); w.a_hi = half_max(q.an ? v.a1 : 0);
+    w.b_lo = half_min(q.bn ? v.b0 : big); w.b_hi = half_max(q.bn ? v.b1 : 0);
+    w.a0_max = half_max(q.valid ? v.a0 : 0); w.a1_min = half_min(q.valid ? v.a1 : big);
+    w.b0_max = half_max(q.valid ? v.b0 : 0); w.b1_min = half_min(q.valid ? v.b1 : big);
+    return q;
+}
+__device__ __forceinline__ bool all_see(const Reach& w, int k0, int k1) {   // keys k0 .. k1 - 1, every query
+    return (w.b0_max <= k0 && k1 <= w.b1_min) || (w.a0_max <= k0 && k1 <= w.a1_min);
+}
+__device__ __forceinline__ bool some_see(const Reach& w, int k0, int k1) {
+    return (k0 < w.b_hi && k1 > w.b_lo) || (k0 < w.a_hi && k1 > w.a_lo);
+}
+
+// The steps of C keys that hold a key which some query sees, in ascending order: two runs of them (prefix, own past), one
+// where they touch.
+struct Steps {
+    int s1, n1, s2, n;
+    __device__ __forceinline__ int at(int i) const { return i < n1 ? s1 + i : s2 + i - n1; }
+};
+template <int C>
+__device__ __forceinline__ Steps steps_of(const Reach& w) {
+    const int sa = w.a_hi > 0 ? w.a_lo / C : 0, ea = w.a_hi > 0 ? (w.a_hi + C - 1) / C : 0;
+    const int sb = w.b_hi > 0 ? w.b_lo / C : 0, eb = w.b_hi > 0 ? (w.b_hi + C - 1) / C : 0;
+    Steps t;
+    if (ea == 0) { t.s1 = sb; t.n1 = t.n = eb - sb; t.s2 = 0; return t; }
+    if (eb == 0) { t.s1 = sa; t.n1 = t.n = ea - sa; t.s2 = 0; return t; }
+    if (sb <= ea && sa <= eb) {   // they overlap or touch
+        t.s1 = sa < sb ? sa : sb;
+        t.n1 = t.n = (ea > eb ? ea : eb) - t.s1;
+        t.s2 = 0;
+        return t;
+    }
+    const bool first = ea < sb;
+    t.s1 = first ? sa : sb; t.n1 = first ? ea - sa : eb - sb;
+    t.s2 = first ? sb : sa; t.n = t.n1 + (first ? eb - sb : ea - sa);
+    return t;
+}
+
+// A row's values as PARTS bf16 B operands: one for bf16 rows, three for float rows (8 + 8 + 8 bits: all of them).
+template <int HD, int PARTS>
+__device__ __forceinline__ void load_query(const PagedAttnArgs& a, const Query& q, int lh, bf16x8 (&op)[PARTS][HD / 16]) {
+    const int64_t at = (int64_t)q.row * a.ld_q + q.head * HD + lh * 8;
+    if constexpr (PARTS == 1) {
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(a.q) + at;
+#pragma unroll
+        for (int ks = 0; ks < HD / 16; ++ks) op[0][ks] = *reinterpret_cast<const bf16x8*>(p + ks * 16);
+    } else {
+        const float* p = reinterpret_cast<const float*>(a.q) + at;
+#pragma unroll
+        for (int ks = 0; ks < HD / 16; ++ks) {
+            const float4 x = *reinterpret_cast<const float4*>(p + ks * 16), y = *reinterpret_cast<const float4*>(p + ks * 16 + 4);
+            float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    w[e] = pack_bf16(f[2 * e], f[2 * e + 1]);
+                    f[2 * e] -= __uint_as_float(w[e] << 16);
+                    f[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+                }
+                op[i][ks] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+            }
+        }
+    }
+}
+
+// Register r of a key tile's scores in lane (li, lh): query li, key key0 + 16 (r / 8) + 8 lh + r % 8.
+__device__ __forceinline__ int reg_key(int r) { return (r >> 3) * 16 + (r & 7); }
+
+// Cap and bias, where there are any: scores in units of log 2 then, raw products else.
+template <int PARTS, int KT>
+__device__ __forceinline__ void shape_scores(const PagedAttnArgs& a, const Query& q, int key0, int lh, f32x16 (&st)[KT]) {
+    if (a.cap > 0.f) {
+        const float c2 = a.cap * LOG2E;
+        if constexpr (PARTS == 1) {   // tanh x = 1 - 2 / (exp 2x + 1): 2e-7 off at most, of scores that bf16 rows gave
+            const float k = 2.f * LOG2E * a.scale / a.cap;
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    st[t][r] = fmaf(-2.f * c2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(st[t][r] * k) + 1.f), c2);
+        } else {
+            const float k = a.scale / a.cap;
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st[t][r] = c2 * tanhf(st[t][r] * k);
+        }
+    } else if (a.slopes) {
+        const float c2 = a.scale * LOG2E;
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) st[t][r] *= c2;
+    }
+    if (a.slopes) {
+        const float d0 = (float)(q.pos - key0 - 8 * lh);
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) st[t][r] = fmaf(-q.slope2, fabsf(d0 - (float)(32 * t + reg_key(r))), st[t][r]);
+    }
+}
+__device__ __forceinline__ float score_mul(const PagedAttnArgs& a) { return a.cap > 0.f || a.slopes ? 1.f : a.scale * LOG2E; }
+
+template <int KT>
+__device__ __forceinline__ void mask_scores(const Query& q, const Reach& w, int key0, int lh, f32x16 (&st)[KT]) {
+    const uint32_t db = (uint32_t)(key0 + 8 * lh - q.b0), da = (uint32_t)(key0 + 8 * lh - q.a0);
+    if (w.a_hi == 0) {   // (no query of the wave has a prefix)
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (db + (uint32_t)(32 * t + reg_key(r)) >= q.bn) st[t][r] = -SB_INF;
+    } else {
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const uint32_t k = 32 * t + reg_key(r);
+                if (db + k >= q.bn && da + k >= q.an) st[t][r] = -SB_INF;
+            }
+    }
+}
+
+// Running soft-max over KT key tiles of this lane's query (what it does not see is -inf): exponentials as PARTS bf16 B operands
+// of 16 keys each, this lane's part of their sum (of the float values), the output rescaled where needed.  The reference
+// point follows the maximum only when that has grown by more than 2^8 (any reference gives the same quotient).
+template <int PARTS, int KT, int DT>
+__device__ __forceinline__ void soft_max(f32x16 (&st)[KT], float mul, f32x16 (&o)[DT], float& m_run, float& l_run, bf16x8 (&p)[PARTS][2 * KT]) {
+    float mx = -SB_INF;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[kt][r]);
+    mx = lanes_max<32, 32>(mx) * mul;
+    const float m_new = mx > m_run + 8.0f ? mx : m_run;
+    const bool large = fabsf(mx) > 1e6f && mx != -SB_INF;
+    if (__builtin_amdgcn_ballot_w64(large) != 0) {
+        // (the reference point is a rounded product, and the exponents below are not: with such scores they would be far from 0 at the maximum)
+        const float f = large ? mul : 1.f;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) st[kt][r] *= f;
+        mul = large ? 1.f : mul;
+    }
+    if (__builtin_amdgcn_ballot_w64(m_new != m_run) != 0) {
+        const float alpha = m_new == m_run ? 1.0f : __builtin_amdgcn_exp2f(m_run - m_new);
+        l_run *= alpha;
+        m_run = m_new;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+    }
+    const float ref = m_new == -SB_INF ? 0.f : m_new;   // (nothing seen so far)
+    float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+    for (int s = 0; s < KT * 2; ++s) {
+        uint32_t w[PARTS][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float p0 = __builtin_amdgcn_exp2f(fmaf(st[s >> 1][(s & 1) * 8 + 2 * e], mul, -ref));
+            float p1 = __builtin_amdgcn_exp2f(fmaf(st[s >> 1][(s & 1) * 8 + 2 * e + 1], mul, -ref));
+            sum0 += p0;
+            sum1 += p1;
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) {
+                w[i][e] = pack_bf16(p0, p1);
+                p0 -= __uint_as_float(w[i][e] << 16);
+                p1 -= __uint_as_float(w[i][e] & 0xffff0000u);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) p[i][s] = __builtin_bit_cast(bf16x8, make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]));
+    }
+    l_run += sum0 + sum1;
+}
+
+// Among eight bf16 values an infinity or NaN is one with all exponent bits set: the largest magnitudes so far, pairwise.
+__device__ __forceinline__ void most(uint4 v, u16x2v& top) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2v, w[e] & 0x7fff7fffu));
+}
+__device__ __forceinline__ bool not_finite(u16x2v top) { return __builtin_amdgcn_ballot_w64(top.x >= 0x7f80 || top.y >= 0x7f80) != 0; }
+
+// Where some value is infinite or NaN and not every query sees its key, the product must not be taken as it is (0 x NaN is not 0):
+// the value becomes zero, and the largest float stands in `bad` for it (zero for all others).  bad x sight, with the largest
+// float in `sight` for the keys that a query sees, is infinite for the queries that see the value and zero for the others.
+__device__ __forceinline__ void set_apart(uint4& v, uint4& bad) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w}, n[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        n[e] = ((w[e] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+        w[e] &= ~n[e];
+        n[e] &= 0x7f7f7f7fu;
+    }
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+    bad = make_uint4(n[0], n[1], n[2], n[3]);
+}
+__device__ __forceinline__ bf16x8 sight(const Query& q, int key) {   // of keys key .. key + 7
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t k = key + e;
+        if (k - q.b0 < q.bn || k - q.a0 < q.an) w[e >> 1] |= e & 1 ? 0x7f7f0000u : 0x7f7fu;
+    }
+    return __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+}
+
+template <int HD>
+__device__ __forceinline__ void store_out4(const PagedAttnArgs& a, const Query& q, int col, float4 v) {
+    const int64_t at = (int64_t)q.row * a.ld_out + q.head * HD + col;
+    if (a.x_dtype == SB_FP32) *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at) = v;
+    else *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+}
+
+// Partial results of a (row, head) pair's key chunks, where the key axis is split over blocks: outputs, then {reference point,
+// sum}, then the number of chunks.
+struct Partials {
+    float *o, *ml;
+    int* count;
+    __host__ __device__ Partials(float* scratch, int64_t pairs, int chunks, int hd) {
+        o = scratch;
+        ml = o + pairs * chunks * hd;
+        count = reinterpret_cast<int*>(ml + pairs * chunks * 2);
+    }
+    static size_t bytes(int64_t pairs, int chunks, int hd) { return ((size_t)pairs * chunks * (hd + 2) + pairs) * 4; }
+};
+
+// A block owns 32 queries of one kv head and (blockIdx.y) `steps_per_chunk` of the 32-key steps that they see; its four waves take the steps in
+// turn with a running soft-max each, operands straight from the cache into registers, the next step's keys requested when
+// this step's scores are done and its values when its products are; the waves' results are added in wave order through LDS.
+template <int HD, int PARTS>
+__global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void paged_attn_apart_kernel(PagedAttnArgs a, int steps_per_chunk) {
+    constexpr int W = 4, KS = HD / 16, DT = HD / 32, SLAB = SB_KV_BLOCK * HD, NS = DT * 4;
+    __shared__ __attribute__((aligned(16))) float o_s[W][NS][64][4];
+    __shared__ float m_s[W][32], l_s[W][32];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int li = lane & 31, lh = lane >> 5;
+    const int Hkv = a.kv.n_kv_heads, g = blockIdx.x % Hkv;
+    int q0;
+    const SeqRows s = tile_seq<32>(a, blockIdx.x / Hkv, q0);
+    if (s.b < 0) return;
+    Reach w;
+    const Query q = lane_query(a, s, g, q0 + li, w);
+    const Steps steps = steps_of<32>(w);
+    const bool split = gridDim.y > 1;
+    const Partials part(a.scratch, (int64_t)a.kv.n_rows * a.n_heads, gridDim.y, HD);
+    const int64_t pair = (int64_t)q.row * a.n_heads + q.head;
+    const int first = blockIdx.y * steps_per_chunk;
+    if (split && blockIdx.y == 0 && wave == 0 && lh == 0 && q.valid) part.count[pair] = (steps.n + steps_per_chunk - 1) / steps_per_chunk;
+    if (first >= steps.n && (split || blockIdx.y > 0)) return;
+    const int last = first + steps_per_chunk < steps.n ? first + steps_per_chunk : steps.n;
+
+    const int64_t page_elems = (int64_t)Hkv * SLAB;
+    const uint16_t* const kbase = a.kv.k + (int64_t)g * SLAB;
+    const uint16_t* const vbase = a.kv.v + (int64_t)g * SLAB;
+    const int32_t* const table = a.kv.table + (int64_t)s.b * a.kv.table_ld;
+    const int krow = (li & 19) | ((li & 4) << 1) | ((li & 8) >> 1);   // row li of a tile is key krow of it
+    const uint32_t koff = (uint32_t)((krow & 15) * HD + lh * 8), voff = (uint32_t)(li * SB_KV_BLOCK + lh * 8);
+    uint4 kr[KS], vr[2][DT];
+    int pg0 = 0, pg1 = 0;   // pages of the step whose operands are requested next; -1: none (nothing is read, zeros)
+    auto lookup = [&](int i) {
+        const int t = steps.at(i);
+        pg0 = table[2 * t];
+        pg1 = (2 * t + 1) * SB_KV_BLOCK < s.len ? table[2 * t + 1] : -1;
+        if (pg0 >= a.kv.n_pages) pg0 = -1;
+        if (pg1 >= a.kv.n_pages) pg1 = -1;
+    };
+    auto load_k = [&]() {
+        const int pg = li & 16 ? pg1 : pg0;
+        const uint16_t* p = kbase + (pg < 0 ? 0 : pg) * page_elems + koff;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kr[ks] = *reinterpret_cast<const uint4*>(p + ks * 16);
+    };
+    auto load_v = [&](int p0, int p1) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int pg = x ? p1 : p0;
+            const uint16_t* p = vbase + (pg < 0 ? 0 : pg) * page_elems + voff;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) vr[x][dt] = *reinterpret_cast<const uint4*>(p + dt * 32 * SB_KV_BLOCK);
+        }
+    };
+    int i = first + wave;
+    const bool any = i < last;
+    int cp0 = 0, cp1 = 0;   // pages of the step being worked on
+    if (any) {
+        lookup(i);
+        load_k();
+        load_v(pg0, pg1);
+        cp0 = pg0; cp1 = pg1;
+        if (i + W < last) lookup(i + W);
+    }
+    bf16x8 qo[PARTS][KS];
+    load_query<HD, PARTS>(a, q, lh, qo);
+    const float mul = score_mul(a);
+    f32x16 o[DT];
+    float m_run = -SB_INF, l_run = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
+    for (; i < last; i += W) {
+        const int key0 = steps.at(i) * 32;
+        if (cp0 < 0 || cp1 < 0) {   // (uniform) keys without a page: zeros
+            const bool none = (li & 16 ? cp1 : cp0) < 0;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+                if (none) kr[ks] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                if (cp0 < 0) vr[0][dt] = make_uint4(0, 0, 0, 0);
+                if (cp1 < 0) vr[1][dt] = make_uint4(0, 0, 0, 0);
+            }
+        }
+        f32x16 st[1];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st[0][r] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int x = 0; x < PARTS; ++x) st[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[ks]), qo[x][ks], st[0], 0, 0, 0);
+        const bool more = i + W < last;
+        const int np0 = pg0, np1 = pg1;
+        if (more) {
+            load_k();
+            if (i + 2 * W < last) lookup(i + 2 * W);
+        }
+        shape_scores<PARTS, 1>(a, q, key0, lh, st);
+        const bool masked = !all_see(w, key0, key0 + 32);
+        if (masked) mask_scores<1>(q, w, key0, lh, st);
+        if (key0 + 32 > s.len) {   // slots past the last key
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int live = s.len - key0 - 16 * x - 8 * lh;   // keys of this lane's 8 that exist
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    uint32_t u[4] = {vr[x][dt].x, vr[x][dt].y, vr[x][dt].z, vr[x][dt].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) u[e] = 2 * e + 1 < live ? u[e] : (2 * e < live ? u[e] & 0xffffu : 0u);
+                    vr[x][dt] = make_uint4(u[0], u[1], u[2], u[3]);
+                }
+            }
+        }
+        bf16x8 p[PARTS][2];
+        soft_max<PARTS, 1, DT>(st, mul, o, m_run, l_run, p);
+        bool sick = false;
+        if (masked) {
+            u16x2v top = {0, 0};
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) most(vr[x][dt], top);
+            sick = not_finite(top);
+        }
+        if (sick) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const bf16x8 see = sight(q, key0 + 16 * x + 8 * lh);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    uint4 bad;
+                    set_apart(vr[x][dt], bad);
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, bad), see, o[dt], 0, 0, 0);
+                }
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int y = 0; y < PARTS; ++y)
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vr[x][dt]), p[y][x], o[dt], 0, 0, 0);
+        if (more) load_v(np0, np1);
+        cp0 = np0; cp1 = np1;
+    }
+    // ---- the waves' results, brought to one reference point and added in wave order
+    l_run = lanes_sum<32, 32>(l_run);
+    if (lh == 0) { m_s[wave][li] = m_run; l_s[wave][li] = l_run; }
+    __syncthreads();
+    float mx = m_s[0][li];
+#pragma unroll
+    for (int v = 1; v < W; ++v) mx = fmaxf(mx, m_s[v][li]);
+    const float ref = mx == -SB_INF ? 0.f : mx;
+    float l = 0.f;
+#pragma unroll
+    for (int v = 0; v < W; ++v) l += l_s[v][li] * __builtin_amdgcn_exp2f(m_s[v][li] - ref);
+    const float f = __builtin_amdgcn_exp2f(m_run - ref);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            *reinterpret_cast<f32x4*>(o_s[wave][dt * 4 + r / 4][lane]) = f32x4{o[dt][r] * f, o[dt][r + 1] * f, o[dt][r + 2] * f, o[dt][r + 3] * f};
+    __syncthreads();
+    if (!q.valid) return;
+    const float inv_l = split ? 1.f : l == 0.f ? 0.f : 1.0f / l;
+    const int64_t at = pair * gridDim.y + blockIdx.y;
+    if (split && wave == 0 && lh == 0) { part.ml[2 * at] = mx; part.ml[2 * at + 1] = l; }
+    for (int n = wave; n < NS; n += W) {   // (a lane finishes its own query: slot n holds dims 32 (n / 4) + 8 (n % 4) + 4 lh ..)
+        f32x4 v = *reinterpret_cast<const f32x4*>(o_s[0][n][lane]);
+#pragma unroll
+        for (int x = 1; x < W; ++x) {
+            const f32x4 u = *reinterpret_cast<const f32x4*>(o_s[x][n][lane]);
+            v[0] += u[0]; v[1] += u[1]; v[2] += u[2]; v[3] += u[3];
+        }
+        const int col = (n >> 2) * 32 + (n & 3) * 8 + 4 * lh;
+        const float4 r = make_float4(v[0] * inv_l, v[1] * inv_l, v[2] * inv_l, v[3] * inv_l);
+        if (split) *reinterpret_cast<float4*>(part.o + at * HD + col) = r;
+        else store_out4<HD>(a, q, col, r);
+    }
+}
+
+// A block per (row, head): its chunks' results at one reference point, added in a fixed order.
+template <int HD>
+__global__ __launch_bounds__(256) void paged_attn_merge_kernel(PagedAttnArgs a, int chunks) {
+    constexpr int L = HD / 4, NG = 256 / L;   // lanes (four dims each) of a group, groups
+    __shared__ float red[4];
+    __shared__ float ls[NG];
+    __shared__ __attribute__((aligned(16))) float os[NG][HD];
+    const int tid = threadIdx.x, row = blockIdx.x / a.n_heads, head = blockIdx.x % a.n_heads, grp = tid / L, d = tid % L * 4;
+    const SeqRows s = seq_rows(a.kv, __builtin_amdgcn_readfirstlane(find_seq(a.kv.n_seq, [&](int b) { return row_at(a.kv, b); }, row)));
+    if (s.b < 0 || row >= s.r0 + s.n) return;
+    const Partials part(a.scratch, (int64_t)a.kv.n_rows * a.n_heads, chunks, HD);
+    const int64_t pair = blockIdx.x, at = pair * chunks;
+    const int n = part.count[pair];
+    float mx = -SB_INF;
+    for (int c = tid; c < n; c += 256) mx = fmaxf(mx, part.ml[2 * (at + c)]);
+    mx = wave_max(mx);
+    if ((tid & 63) == 0) red[tid >> 6] = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float ref = mx == -SB_INF ? 0.f : mx;
+    float l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int c = grp; c < n; c += NG) {
+        const float2 ml = *reinterpret_cast<const float2*>(part.ml + 2 * (at + c));
+        const float4 v = *reinterpret_cast<const float4*>(part.o + (at + c) * HD + d);
+        const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+        l += ml.y * f;
+        o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+    }
+    *reinterpret_cast<float4*>(&os[grp][d]) = o;
+    if (d == 0) ls[grp] = l;
+    __syncthreads();
+    if (tid >= HD) return;
+    float t = 0.f, v = 0.f;
+#pragma unroll
+    for (int x = 0; x < NG; ++x) { t += ls[x]; v += os[x][tid]; }
+    store_x(a.out, (int64_t)row * a.ld_out + head * HD + tid, a.x_dtype == SB_FP32, t == 0.f ? 0.f : v / t);
+}
+
+// How the keys of a call are split: 32-key steps per block (a multiple of the four waves) and the most chunks that gives.
+struct AttnPlan { int64_t tiles; int steps, chunks; };
+static AttnPlan attn_plan(const PagedKv& kv, int32_t n_heads) {
+    const int64_t G = n_heads / kv.n_kv_heads, total = (kv.max_len + 31) / 32;
+    AttnPlan p;
+    p.tiles = kv.n_rows * G / 32 + kv.n_seq;
+    const int64_t want = (p.tiles * kv.n_kv_heads * total + 2047) / 2048;
+    p.steps = (int)(want < 4 ? 4 : want > 64 ? 64 : (want + 3) / 4 * 4);
+    if (p.tiles * kv.n_kv_heads >= 1024) p.steps = (int)((total + 3) / 4 * 4);
+    if (total / p.steps > 512) p.steps = (int)((total / 512 + 3) / 4 * 4);
+    p.chunks = (int)((total + p.steps - 1) / p.steps);
+    return p;
+}
+
+size_t paged_attention_scratch(const PagedKv& kv, int32_t n_heads) {
+    const AttnPlan p = attn_plan(kv, n_heads);
+    return p.chunks > 1 ? Partials::bytes((int64_t)kv.n_rows * n_heads, p.chunks, kv.head_dim) : 0;
+}
 
 hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t st) {
-    const dim3 grid(a.kv.n_rows, a.n_heads);
-    return a.kv.head_dim == 128 ? launch(&paged_attn_kernel<128>, grid, 64, st, a) : launch(&paged_attn_kernel<64>, grid, 64, st, a);
+    const AttnPlan p = attn_plan(a.kv, a.n_heads);
+    const auto go = [&](auto hd_c) {
+        constexpr int HD = decltype(hd_c)::value;
+        const dim3 grid((unsigned)(p.tiles * a.kv.n_kv_heads), p.chunks);
+        const hipError_t e = launch(a.x_dtype == SB_FP32 ? &paged_attn_apart_kernel<HD, 3> : &paged_attn_apart_kernel<HD, 1>, grid, 256, st, a, p.steps);
+        if (e != hipSuccess || p.chunks == 1) return e;
+        return launch(&paged_attn_merge_kernel<HD>, dim3(a.kv.n_rows * a.n_heads), 256, st, a, p.chunks);
+    };
+    return a.kv.head_dim == 128 ? go(std::integral_constant<int, 128>{}) : go(std::integral_constant<int, 64>{});
 }
 
 // ---------------------------------------------------------------- page copies
