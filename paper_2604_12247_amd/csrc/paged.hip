@@ -51,58 +51,167 @@ __device__ __forceinline__ void store_x(void* x, int64_t i, bool fp32, float v) 
 }
 
 // ---------------------------------------------------------------- rotary append
-// A wave per row and head, grid (rows, ceil(heads / 4)).
-template <int HD>
-__global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a) {
-    __shared__ float xs[4][HD];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x;
-    const int Hq = a.n_heads, Hkv = a.kv.n_kv_heads, head = blockIdx.y * 4 + wave;
-    const SeqRows s = seq_rows(a.kv, find_seq(a.kv.n_seq, [&](int b) { return row_at(a.kv, b); }, row));
-    const int pos = s.len - s.n + row - s.r0, rot = a.rot_dim, half = rot / 2;
-    const bool fp32 = a.x_dtype == SB_FP32;
-    const bool on = s.b >= 0 && row < s.r0 + s.n && head < Hq + 2 * Hkv && pos >= 0 && (rot == 0 || pos < a.n_pos);
-    const bool is_v = head >= Hq + Hkv;
-    const float* gain = head < Hq ? a.q_gain : is_v ? nullptr : a.k_gain;
-    float x[HD / 64], ss = 0.f;
-    if (on) {
-        for (int i = 0; i < HD / 64; ++i) {
-            x[i] = load_x(a.qkv, (int64_t)row * a.ld_qkv + head * HD + i * 64 + lane, fp32);
-            ss += x[i] * x[i];
-        }
-        if (gain) {
-            const float inv = 1.0f / sqrtf(wave_sum(ss) / (float)HD + a.eps);
-            for (int i = 0; i < HD / 64; ++i) x[i] = x[i] * inv * gain[i * 64 + lane];
-        }
-        for (int i = 0; i < HD / 64; ++i) xs[wave][i * 64 + lane] = x[i];
-    }
-    __syncthreads();
-    if (!on) return;
-    const int page = pos / SB_KV_BLOCK, slot = pos % SB_KV_BLOCK;
+// Four neighbouring values of a row.
+__device__ __forceinline__ void load4(const float* p, float (&x)[4]) {
+    const float4 v = *reinterpret_cast<const float4*>(p);
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+}
+__device__ __forceinline__ void load4(const uint16_t* p, float (&x)[4]) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xffff0000u);
+    x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xffff0000u);
+}
+__device__ __forceinline__ void store4(float* p, const float (&x)[4]) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ void store4(uint16_t* p, const float (&x)[4]) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])); }
+// Two, rounded to a pair of bf16.
+__device__ __forceinline__ uint32_t load_pair(const float* p) {
+    const float2 v = *reinterpret_cast<const float2*>(p);
+    return pack_bf16(v.x, v.y);
+}
+__device__ __forceinline__ uint32_t load_pair(const uint16_t* p) { return *reinterpret_cast<const uint32_t*>(p); }
+
+// A block takes the new rows of one page of one sequence (16 at most) and, by blockIdx.y, some of the heads: ROPE_QK q and k
+// heads, or ROPE_V v heads.  Sequence b's pages are tiles row_start[b] / 16 + 2 b .., as many as its rows can touch.
+//   q and k: HD / 8 lanes a head, eight values a lane -- the two ends of four pairs, so that norm and rotation stay within
+// the lane but for the sum of squares; ROPE_U heads a thread in flight.
+//   v: a thread takes two dims and eight slots, and its page half leaves as 16-byte pieces of the transposed slab where all
+// eight are new.
+constexpr int ROPE_QK = 16, ROPE_V = 8, ROPE_U = 4;
+
+template <int HD, typename XT>
+__global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a, int qk_slices) {
+    const int tid = threadIdx.x, Hq = a.n_heads, Hkv = a.kv.n_kv_heads, rot = a.rot_dim, half = rot / 2;
+    const int t = blockIdx.x;
+    const auto first = [&](int b) { return row_at(a.kv, b) / SB_KV_BLOCK + 2 * b; };
+    const int b = __builtin_amdgcn_readfirstlane(find_seq(a.kv.n_seq, first, t));
+    const SeqRows s = seq_rows(a.kv, b);
+    if (s.b < 0) return;
+    const int pos0 = s.len - s.n, from = pos0 > 0 ? pos0 : 0;
+    const int page = from / SB_KV_BLOCK + t - (s.r0 / SB_KV_BLOCK + 2 * b);
+    const int lo = page * SB_KV_BLOCK > from ? page * SB_KV_BLOCK : from;
+    int hi = (page + 1) * SB_KV_BLOCK < s.len ? (page + 1) * SB_KV_BLOCK : s.len;
+    if (rot && hi > a.n_pos) hi = a.n_pos;
+    if (lo >= hi) return;
+    const int nr = hi - lo, row0 = s.r0 + lo - pos0;   // rows row0 .. at positions lo ..
     const int pg = a.kv.table[(int64_t)s.b * a.kv.table_ld + page];
-    for (int i = 0; i < HD / 64; ++i) {
-        const int d = i * 64 + lane;
-        float y = x[i];
-        if (!is_v && d < rot) {
-            const bool second = a.interleaved ? d & 1 : d >= half;
-            const int p = a.interleaved ? d >> 1 : second ? d - half : d;
-            const float o = xs[wave][a.interleaved ? d ^ 1 : second ? d - half : d + half];
-            const float c = a.cos[(int64_t)pos * half + p], n = a.sin[(int64_t)pos * half + p];
-            y = second ? x[i] * c + o * n : x[i] * c - o * n;
+    const bool in_pool = pg >= 0 && pg < a.kv.n_pages;
+    const XT* const x = reinterpret_cast<const XT*>(a.qkv);
+    const int64_t slab = (int64_t)(in_pool ? pg : 0) * Hkv * SB_KV_BLOCK * HD;
+
+    if ((int)blockIdx.y < qk_slices) {
+        constexpr int L = HD / 8, SIDE = 256 / L;
+        const int c = tid % L, h0 = blockIdx.y * ROPE_QK;
+        const int nh = Hq + Hkv - h0 < ROPE_QK ? Hq + Hkv - h0 : ROPE_QK, n = nr * nh;
+        const bool turns = c < rot / 8;
+        const int dA = a.interleaved ? 8 * c : turns ? 4 * c : rot + 8 * (c - rot / 8);
+        const int dB = a.interleaved || !turns ? dA + 4 : dA + half;
+        for (int i0 = tid / L; i0 < n; i0 += SIDE * ROPE_U) {
+            float u[ROPE_U][2][4];
+            int head[ROPE_U], r[ROPE_U];
+#pragma unroll
+            for (int k = 0; k < ROPE_U; ++k) {   // (past the end: the last one again, not stored)
+                const int i = i0 + k * SIDE < n ? i0 + k * SIDE : n - 1;
+                r[k] = i / nh;
+                head[k] = h0 + i - r[k] * nh;
+                const XT* p = x + (row0 + r[k]) * a.ld_qkv + head[k] * HD;
+                load4(p + dA, u[k][0]);
+                load4(p + dB, u[k][1]);
+            }
+#pragma unroll
+            for (int k = 0; k < ROPE_U; ++k) {
+                float (&A)[4] = u[k][0], (&B)[4] = u[k][1];
+                const bool is_q = head[k] < Hq;
+                const float* gain = is_q ? a.q_gain : a.k_gain;
+                if (a.q_gain || a.k_gain) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) ss += A[e] * A[e] + B[e] * B[e];
+                    ss = lanes_sum<L / 2>(ss);
+                    if (gain) {
+                        const float inv = 1.0f / sqrtf(ss * (1.0f / HD) + a.eps);
+                        float ga[4], gb[4];
+                        load4(gain + dA, ga);
+                        load4(gain + dB, gb);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { A[e] = A[e] * inv * ga[e]; B[e] = B[e] * inv * gb[e]; }
+                    }
+                }
+                if (turns) {
+                    float cs[4], sn[4];
+                    load4(a.cos + (int64_t)(lo + r[k]) * half + 4 * c, cs);
+                    load4(a.sin + (int64_t)(lo + r[k]) * half + 4 * c, sn);
+                    if (a.interleaved) {   // pairs are neighbours: (A0, A1), (A2, A3), (B0, B1), (B2, B3)
+#pragma unroll
+                        for (int e = 0; e < 4; e += 2) {
+                            const float a0 = A[e], a1 = A[e + 1], b0 = B[e], b1 = B[e + 1];
+                            A[e] = a0 * cs[e / 2] - a1 * sn[e / 2]; A[e + 1] = a1 * cs[e / 2] + a0 * sn[e / 2];
+                            B[e] = b0 * cs[2 + e / 2] - b1 * sn[2 + e / 2]; B[e + 1] = b1 * cs[2 + e / 2] + b0 * sn[2 + e / 2];
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float v = A[e], w = B[e];
+                            A[e] = v * cs[e] - w * sn[e];
+                            B[e] = w * cs[e] + v * sn[e];
+                        }
+                    }
+                }
+                if (i0 + k * SIDE >= n) continue;
+                if (is_q) {
+                    XT* p = reinterpret_cast<XT*>(a.q_out) + (row0 + r[k]) * a.ld_q + head[k] * HD;
+                    store4(p + dA, A);
+                    store4(p + dB, B);
+                } else if (in_pool) {
+                    uint16_t* p = a.kv.k + slab + ((head[k] - Hq) * SB_KV_BLOCK + (lo + r[k]) % SB_KV_BLOCK) * HD;
+                    store4(p + dA, A);
+                    store4(p + dB, B);
+                }
+            }
         }
-        if (head < Hq) {
-            store_x(a.q_out, (int64_t)row * a.ld_q + head * HD + d, fp32, y);
-        } else if (pg >= 0 && pg < a.kv.n_pages) {
-            const int g = is_v ? head - Hq - Hkv : head - Hq;
-            const int64_t slab = ((int64_t)pg * Hkv + g) * SB_KV_BLOCK * HD;
-            if (is_v) a.kv.v[slab + d * SB_KV_BLOCK + slot] = round_bf16(y);
-            else a.kv.k[slab + slot * HD + d] = round_bf16(y);
+        return;
+    }
+    if (!in_pool) return;
+    const int g0 = (blockIdx.y - qk_slices) * ROPE_V, ng = Hkv - g0 < ROPE_V ? Hkv - g0 : ROPE_V;
+    const int s_lo = lo % SB_KV_BLOCK, s_hi = s_lo + nr;   // new slots of the page
+    for (int i = tid; i < ng * HD; i += 256) {
+        const int g = g0 + i / HD, d = i % HD & ~1, t0 = (i & 1) * 8;
+        if (t0 >= s_hi || t0 + 8 <= s_lo) continue;
+        const XT* p = x + (Hq + Hkv + g) * HD + d;
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {   // (no condition, so the eight go out together)
+            const int sl = t0 + e < s_lo ? s_lo : t0 + e < s_hi ? t0 + e : s_hi - 1;
+            w[e] = load_pair(p + (row0 + sl - s_lo) * a.ld_qkv);
+        }
+        uint16_t* dst = a.kv.v + slab + (g * HD + d) * SB_KV_BLOCK + t0;
+        if (t0 >= s_lo && t0 + 8 <= s_hi) {
+            uint32_t lo2[4], hi2[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                lo2[e] = (w[2 * e] & 0xffffu) | (w[2 * e + 1] << 16);
+                hi2[e] = (w[2 * e] >> 16) | (w[2 * e + 1] & 0xffff0000u);
+            }
+            *reinterpret_cast<uint4*>(dst) = make_uint4(lo2[0], lo2[1], lo2[2], lo2[3]);
+            *reinterpret_cast<uint4*>(dst + SB_KV_BLOCK) = make_uint4(hi2[0], hi2[1], hi2[2], hi2[3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (t0 + e >= s_lo && t0 + e < s_hi) {
+                    dst[e] = (uint16_t)w[e];
+                    dst[SB_KV_BLOCK + e] = (uint16_t)(w[e] >> 16);
+                }
         }
     }
 }
 
 hipError_t launch_rope_append(const RopeAppendArgs& a, hipStream_t st) {
-    const dim3 grid(a.kv.n_rows, (a.n_heads + 2 * a.kv.n_kv_heads + 3) / 4);
-    return a.kv.head_dim == 128 ? launch(&rope_append_kernel<128>, grid, 256, st, a) : launch(&rope_append_kernel<64>, grid, 256, st, a);
+    const int qk = (a.n_heads + a.kv.n_kv_heads + ROPE_QK - 1) / ROPE_QK, v = (a.kv.n_kv_heads + ROPE_V - 1) / ROPE_V;
+    const dim3 grid(a.kv.n_rows / SB_KV_BLOCK + 2 * a.kv.n_seq, qk + v);
+    const auto go = [&](auto hd_c) {
+        constexpr int HD = decltype(hd_c)::value;
+        return launch(a.x_dtype == SB_FP32 ? &rope_append_kernel<HD, float> : &rope_append_kernel<HD, uint16_t>, grid, 256, st, a, qk);
+    };
+    return a.kv.head_dim == 128 ? go(std::integral_constant<int, 128>{}) : go(std::integral_constant<int, 64>{});
 }
 
 // ---------------------------------------------------------------- attention
@@ -660,14 +769,29 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------- page copies
-// grid (pages, slabs).
-__global__ __launch_bounds__(256) void copy_pages_kernel(CopyPagesArgs a) {
-    const uint4* s = reinterpret_cast<const uint4*>(a.src + blockIdx.y * a.src_slab + a.from[blockIdx.x] * a.page_bytes);
-    uint4* d = reinterpret_cast<uint4*>(a.dst + blockIdx.y * a.dst_slab + a.to[blockIdx.x] * a.page_bytes);
-    for (size_t i = threadIdx.x; i < a.page_bytes / 16; i += 256) d[i] = s[i];
+// A block copies COPY_PIECE bytes of a page, four 16-byte loads a thread in flight.  grid (pages x pieces of a page, slabs).
+constexpr int COPY_PIECE = 16384;
+__global__ __launch_bounds__(256) void copy_pages_kernel(CopyPagesArgs a, int pieces) {
+    const int page = blockIdx.x / pieces, piece = blockIdx.x - page * pieces;
+    const uint4* s = reinterpret_cast<const uint4*>(a.src + blockIdx.y * a.src_slab + a.from[page] * a.page_bytes);
+    uint4* d = reinterpret_cast<uint4*>(a.dst + blockIdx.y * a.dst_slab + a.to[page] * a.page_bytes);
+    const size_t n = a.page_bytes / 16, i = (size_t)piece * (COPY_PIECE / 16) + threadIdx.x;
+    constexpr int U = COPY_PIECE / (16 * 256);
+    if (i + (U - 1) * 256 < n) {
+        uint4 v[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) v[k] = s[i + k * 256];
+#pragma unroll
+        for (int k = 0; k < U; ++k) d[i + k * 256] = v[k];
+    } else {
+        for (int k = 0; k < U; ++k)
+            if (i + k * 256 < n) d[i + k * 256] = s[i + k * 256];
+    }
 }
 hipError_t launch_copy_pages(const CopyPagesArgs& a, int32_t n, int32_t n_slabs, hipStream_t st) {
-    return launch(&copy_pages_kernel, dim3(n, n_slabs), 256, st, a);
+    const size_t pieces = (a.page_bytes + COPY_PIECE - 1) / COPY_PIECE;
+    if (pieces * n > 0x7fffffff) return hipErrorInvalidValue;
+    return launch(&copy_pages_kernel, dim3((unsigned)(pieces * n), n_slabs), 256, st, a, (int)pieces);
 }
 
 }  // namespace sb
