@@ -351,8 +351,9 @@ __device__ __forceinline__ void load_query(const PagedAttnArgs& a, const Query& 
 __device__ __forceinline__ int reg_key(int r) { return (r >> 3) * 16 + (r & 7); }
 
 // Cap and bias, where there are any: scores in units of log 2 then, raw products else.
-template <int PARTS, int KT>
+template <int PARTS, int KT, bool SHAPED>
 __device__ __forceinline__ void shape_scores(const PagedAttnArgs& a, const Query& q, int key0, int lh, f32x16 (&st)[KT]) {
+    if constexpr (!SHAPED) return;
     if (a.cap > 0.f) {
         const float c2 = a.cap * LOG2E;
         if constexpr (PARTS == 1) {   // tanh x = 1 - 2 / (exp 2x + 1): 2e-7 off at most, of scores that bf16 rows gave
@@ -411,11 +412,11 @@ __device__ __forceinline__ void mask_scores(const Query& q, const Reach& w, int 
 // point follows the maximum only when that has grown by more than 2^8 (any reference gives the same quotient).
 template <int PARTS, int KT, int DT>
 __device__ __forceinline__ void soft_max(f32x16 (&st)[KT], float mul, f32x16 (&o)[DT], float& m_run, float& l_run, bf16x8 (&p)[PARTS][2 * KT]) {
-    float mx = -SB_INF;
+    float mx = -SB_INF;   // (the maximum that a NaN passes through: fmaxf first multiplies every score by 1 to quiet it)
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[kt][r]);
+        for (int r = 0; r < 16; r += 2) mx = __builtin_elementwise_maximum(mx, __builtin_elementwise_maximum(st[kt][r], st[kt][r + 1]));
     mx = lanes_max<32, 32>(mx) * mul;
     const float m_new = mx > m_run + 8.0f ? mx : m_run;
     const bool large = fabsf(mx) > 1e6f && mx != -SB_INF;
@@ -613,7 +614,7 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void paged_attn_apart_kern
             load_k();
             if (i + 2 * W < last) lookup(i + 2 * W);
         }
-        shape_scores<PARTS, 1>(a, q, key0, lh, st);
+        shape_scores<PARTS, 1, true>(a, q, key0, lh, st);
         const bool masked = !all_see(w, key0, key0 + 32);
         if (masked) mask_scores<1>(q, w, key0, lh, st);
         if (key0 + 32 > s.len) {   // slots past the last key
@@ -737,11 +738,227 @@ __global__ __launch_bounds__(256) void paged_attn_merge_kernel(PagedAttnArgs a, 
     store_x(a.out, (int64_t)row * a.ld_out + head * HD + tid, a.x_dtype == SB_FP32, t == 0.f ? 0.f : v / t);
 }
 
+// For many rows: a block owns 128 queries of one kv head, 32 a wave, and walks the 64-key steps that any of them sees; the
+// steps' keys and values are staged in LDS for its four waves, two steps deep, by direct global -> LDS loads issued a step ahead (lane l of a
+// wave lands 16 l bytes after the wave's base).  Which piece lands where is chosen so that operand reads are free of bank conflicts: a K piece
+// (key, p) sits at piece p ^ f(key) of its key's row; the two halves (8 keys each) of a V row change places in every second group of 8 dims.
+template <int HD, int PARTS, bool SHAPED>
+__global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void paged_attn_shared_kernel(PagedAttnArgs a) {
+    constexpr int CH = 64, NT = 256, BQ = 128;
+    constexpr int KT = PARTS == 1 ? 2 : 1;   // 32-key tiles whose scores are held at once
+    constexpr int KS = HD / 16, DT = HD / 32, PPK = HD / 8, SLAB = SB_KV_BLOCK * HD, NPG = CH / SB_KV_BLOCK;
+    constexpr int NL = NPG * SLAB / (NT * 8);   // 16-byte pieces per thread, operand and step
+    constexpr int PD = 4;                       // operands are read from LDS PD ahead of their MFMAs
+    __shared__ __attribute__((aligned(16))) uint16_t k_s[2][CH * HD];
+    __shared__ __attribute__((aligned(16))) uint16_t v_s[2][NPG * SLAB];
+    __shared__ int reach_s[4][8];
+    __shared__ int sick_s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int li = lane & 31, lh = lane >> 5;
+    const int Hkv = a.kv.n_kv_heads, tiles = gridDim.x / Hkv;
+    const int g = blockIdx.x % Hkv;
+    int q0;
+    // A prompt's last rows see most: they start first.  Where all blocks are resident at once (two per CU), the second half goes
+    // the other way round, so that a CU's two blocks are a long and a short one.  (The first n_seq are mostly without queries.)
+    const int at = (int)(blockIdx.x / Hkv) - a.kv.n_seq, half = (256 + Hkv - 1) / Hkv, full = tiles - a.kv.n_seq;
+    const SeqRows s = tile_seq<BQ>(a, at >= half && full <= 2 * half ? at - half : full - 1 - at, q0);
+    if (s.b < 0) return;
+    Reach w;
+    const Query q = lane_query(a, s, g, q0 + wave * 32 + li, w);
+    if (lane == 0) {
+        int* const r = reach_s[wave];
+        r[0] = w.a_lo; r[1] = w.b_lo; r[2] = w.a1_min; r[3] = w.b1_min;
+        r[4] = w.a_hi; r[5] = w.b_hi; r[6] = w.a0_max; r[7] = w.b0_max;
+    }
+    if (tid == 0) sick_s = 0;
+    __syncthreads();
+    int e8[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        int v = reach_s[0][k];
+#pragma unroll
+        for (int i = 1; i < 4; ++i) v = k < 4 ? (reach_s[i][k] < v ? reach_s[i][k] : v) : (reach_s[i][k] > v ? reach_s[i][k] : v);
+        e8[k] = __builtin_amdgcn_readfirstlane(v);
+    }
+    const Reach all{e8[0], e8[4], e8[1], e8[5], e8[6], e8[2], e8[7], e8[3]};
+    const Steps steps = steps_of<CH>(all);
+
+    const int64_t page_elems = (int64_t)Hkv * SLAB;
+    const uint16_t* const kbase = a.kv.k + (int64_t)g * SLAB;
+    const uint16_t* const vbase = a.kv.v + (int64_t)g * SLAB;
+    const int32_t* const table = a.kv.table + (int64_t)s.b * a.kv.table_ld;
+    // A wave's 64 pieces lie in one page, so the page is a scalar; lane i < NPG of `pg` holds the i-th page of the step
+    // issued next (-1: no key there, or no such page), read one step ahead of the issue.
+    int pg = -1;
+    auto lookup = [&](int i) {
+        const int page = (i < steps.n ? steps.at(i) : 0) * NPG + (lane & (NPG - 1));
+        pg = i < steps.n && page * SB_KV_BLOCK < s.len ? table[page] : -1;
+        if (pg >= a.kv.n_pages) pg = -1;
+    };
+    // A thread's place within a page is the same for all its pieces: an offset in a register beside a scalar address.
+    const int slot_p = (wave * 64 + lane) % (SB_KV_BLOCK * PPK), key_p = slot_p / PPK;
+    const uint32_t koff = (uint32_t)(key_p * HD + ((slot_p % PPK) ^ (PPK == 16 ? key_p : (key_p >> 1) & 7)) * 8) * 2;
+    const uint32_t voff = (uint32_t)(slot_p ^ ((slot_p >> 4) & 1)) * 16;
+    auto issue = [&](int buf) {
+        uint32_t ko = koff, vo = voff;
+        asm("" : "+v"(ko), "+v"(vo));   // (else base and offset are added outside the loop, and every load adds 64 bits a lane again)
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int slot0 = i * NT + wave * 64;   // the wave's place in LDS
+            const int page = __builtin_amdgcn_readlane(pg, slot0 / (SB_KV_BLOCK * PPK));
+            uint16_t* kw = &k_s[buf][slot0 * 8];
+            uint16_t* vw = &v_s[buf][slot0 * 8];
+            if (page >= 0) {
+                const int64_t base = page * page_elems;
+                __builtin_amdgcn_global_load_lds(reinterpret_cast<const char*>(kbase + base) + ko, kw, 16, 0, 0);
+                __builtin_amdgcn_global_load_lds(reinterpret_cast<const char*>(vbase + base) + vo, vw, 16, 0, 0);
+            } else {
+                *reinterpret_cast<uint4*>(kw + lane * 8) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4*>(vw + lane * 8) = make_uint4(0, 0, 0, 0);
+            }
+        }
+    };
+    if (steps.n > 0) {
+        lookup(0);
+        issue(0);
+        lookup(1);
+    }
+    bf16x8 qo[PARTS][KS];
+    load_query<HD, PARTS>(a, q, lh, qo);
+    const float mul = score_mul(a);
+    f32x16 o[DT];
+    float m_run = -SB_INF, l_run = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
+    const int krow = (li & 19) | ((li & 4) << 1) | ((li & 8) >> 1);   // row li of a key tile is key krow of it
+    const int kswz = PPK == 16 ? (krow & 15) : ((krow >> 1) & 7);
+
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    for (int i = 0; i < steps.n; ++i) {
+        const int key0 = steps.at(i) * CH, buf = i & 1;
+        if (i + 1 < steps.n) {
+            issue(buf ^ 1);
+            lookup(i + 2);
+        }
+        auto v_at = [&](int page, int dt) {   // dims 32 dt + li, keys 8 lh .. of a page of the step
+            const int slot = (dt * 32 + li) * 2 + lh;
+            return *reinterpret_cast<const bf16x8*>(&v_s[buf][page * SLAB + (slot ^ ((slot >> 4) & 1)) * 8]);
+        };
+        if (!all_see(all, key0, key0 + CH)) {
+            // Some query does not see some key: its value must not be an infinity or NaN in the product.  Slots past the last key are
+            // made zeros; if a value that some query sees is one (a thread looks at the pieces that it staged), its product
+            // with who sees it is taken here and a zero left in its place.
+            u16x2v top = {0, 0};
+#pragma unroll
+            for (int k = 0; k < NL; ++k) {
+                const int slot = k * NT + tid;
+                const int vk = key0 + (slot / (SB_KV_BLOCK * PPK)) * SB_KV_BLOCK + ((slot ^ (slot >> 4)) & 1) * 8;   // keys vk .. vk + 7 of one dim
+                uint4 v = *reinterpret_cast<uint4*>(&v_s[buf][slot * 8]);
+                if (vk + 8 > s.len) {
+                    uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) u[e] = vk + 2 * e + 1 < s.len ? u[e] : vk + 2 * e < s.len ? u[e] & 0xffffu : 0u;
+                    v = make_uint4(u[0], u[1], u[2], u[3]);
+                    *reinterpret_cast<uint4*>(&v_s[buf][slot * 8]) = v;
+                }
+                most(v, top);
+            }
+            if (not_finite(top) && lane == 0) sick_s = i + 1;
+            __syncthreads();
+            if (sick_s == i + 1) {
+#pragma unroll 1
+                for (int x = 0; x < NPG; ++x) {
+                    const bf16x8 see = sight(q, key0 + 16 * x + 8 * lh);
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        uint4 v = __builtin_bit_cast(uint4, v_at(x, dt)), bad;
+                        set_apart(v, bad);
+                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, bad), see, o[dt], 0, 0, 0);
+                    }
+                }
+                __syncthreads();
+#pragma unroll 1
+                for (int k = 0; k < NL; ++k) {
+                    uint4* const at = reinterpret_cast<uint4*>(&v_s[buf][(k * NT + tid) * 8]);
+                    uint4 v = *at, bad;
+                    set_apart(v, bad);
+                    *at = v;
+                }
+                __syncthreads();
+            }
+        }
+#pragma unroll 1
+        for (int t0 = 0; t0 < 2; t0 += KT) {   // tiles t0 .. t0 + KT - 1 of the step
+            const int tk = key0 + 32 * t0;
+            if (!some_see(w, tk, tk + 32 * KT)) continue;
+            f32x16 st[KT];
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st[kt][r] = 0.f;
+            bf16x8 op[PD];
+            auto read_k = [&](int n) {   // k step n / KT of tile n % KT
+                op[n % PD] = *reinterpret_cast<const bf16x8*>(&k_s[buf][(((t0 + n % KT) * 32 + krow) * PPK + (((n / KT) * 2 + lh) ^ kswz)) * 8]);
+            };
+#pragma unroll
+            for (int n = 0; n < PD; ++n) read_k(n);
+#pragma unroll
+            for (int n = 0; n < KT * KS; n += KT) {
+#pragma unroll
+                for (int x = 0; x < PARTS; ++x)
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt) st[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[(n + kt) % PD], qo[x][n / KT], st[kt], 0, 0, 0);
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+                    if (n + kt + PD < KT * KS) read_k(n + kt + PD);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            shape_scores<PARTS, KT, SHAPED>(a, q, tk, lh, st);
+            if (!all_see(w, tk, tk + 32 * KT)) mask_scores<KT>(q, w, tk, lh, st);
+            auto read_v = [&](int n) { op[n % PD] = v_at(2 * t0 + n / DT, n % DT); };
+#pragma unroll
+            for (int n = 0; n < PD; ++n) read_v(n);
+            bf16x8 p[PARTS][2 * KT];
+            soft_max<PARTS, KT, DT>(st, mul, o, m_run, l_run, p);
+#pragma unroll
+            for (int n = 0; n < 2 * KT * DT; n += 2) {
+#pragma unroll
+                for (int y = 0; y < PARTS; ++y)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) o[(n + x) % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[(n + x) % PD], p[y][n / DT], o[(n + x) % DT], 0, 0, 0);
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    if (n + x + PD < 2 * KT * DT) read_v(n + x + PD);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0);   // this wave's pieces of the next step have landed
+        __syncthreads();                 // ... and everybody's; every wave is done with this step
+    }
+    const float l = lanes_sum<32, 32>(l_run), inv_l = l == 0.f ? 0.f : 1.0f / l;
+    if (!q.valid) return;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            store_out4<HD>(a, q, dt * 32 + 2 * r + 4 * lh, make_float4(o[dt][r] * inv_l, o[dt][r + 1] * inv_l, o[dt][r + 2] * inv_l, o[dt][r + 3] * inv_l));
+}
+
 // How the keys of a call are split: 32-key steps per block (a multiple of the four waves) and the most chunks that gives.
-struct AttnPlan { int64_t tiles; int steps, chunks; };
+struct AttnPlan { bool shared; int64_t tiles; int steps, chunks; };
 static AttnPlan attn_plan(const PagedKv& kv, int32_t n_heads) {
     const int64_t G = n_heads / kv.n_kv_heads, total = (kv.max_len + 31) / 32;
     AttnPlan p;
+    p.shared = (int64_t)kv.n_rows * n_heads / 128 >= 320 && kv.n_rows * G >= 64 * kv.n_seq;
+    if (p.shared) {
+        p.tiles = kv.n_rows * G / 128 + kv.n_seq;
+        p.steps = 0;
+        p.chunks = 1;
+        return p;
+    }
     p.tiles = kv.n_rows * G / 32 + kv.n_seq;
     const int64_t want = (p.tiles * kv.n_kv_heads * total + 2047) / 2048;
     p.steps = (int)(want < 4 ? 4 : want > 64 ? 64 : (want + 3) / 4 * 4);
@@ -761,6 +978,10 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t st) {
     const auto go = [&](auto hd_c) {
         constexpr int HD = decltype(hd_c)::value;
         const dim3 grid((unsigned)(p.tiles * a.kv.n_kv_heads), p.chunks);
+        const bool shaped = a.cap > 0.f || a.slopes;
+        if (p.shared)
+            return launch(a.x_dtype == SB_FP32 ? (shaped ? &paged_attn_shared_kernel<HD, 3, true> : &paged_attn_shared_kernel<HD, 3, false>)
+                                               : (shaped ? &paged_attn_shared_kernel<HD, 1, true> : &paged_attn_shared_kernel<HD, 1, false>), grid, 256, st, a);
         const hipError_t e = launch(a.x_dtype == SB_FP32 ? &paged_attn_apart_kernel<HD, 3> : &paged_attn_apart_kernel<HD, 1>, grid, 256, st, a, p.steps);
         if (e != hipSuccess || p.chunks == 1) return e;
         return launch(&paged_attn_merge_kernel<HD>, dim3(a.kv.n_rows * a.n_heads), 256, st, a, p.chunks);

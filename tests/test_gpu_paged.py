@@ -298,6 +298,9 @@ ATT_SHAPES = [
     ([100, 33, 64], [100, 500, 65], 8, 8, 64),
     ([300], [1111], 16, 4, 128),
     ([700, 257], [700, 400], 40, 40, 64),
+    # enough rows that blocks of 128 queries fill the card
+    ([1500, 1200, 70], [1500, 1333, 900], 16, 4, 64),
+    ([1000, 40, 300], [1601, 41, 777], 32, 16, 128),
 ]
 
 
@@ -318,7 +321,7 @@ RULES = [
 
 
 @pytest.mark.parametrize("fp32", [True, False], ids=["fp32", "bf16"])
-@pytest.mark.parametrize("shape", [3, 4, 6, 8, 9, 10, 11])
+@pytest.mark.parametrize("shape", [3, 4, 6, 8, 9, 10, 11, 12, 13])
 @pytest.mark.parametrize("r", range(len(RULES)), ids=lambda i: "-".join(RULES[i]))
 def test_attention_rules(r, shape, fp32):
     rows, lens, hq, hkv, hd = ATT_SHAPES[shape]
@@ -340,7 +343,7 @@ def test_attention_rules(r, shape, fp32):
 
 
 @pytest.mark.parametrize("fp32", [True, False], ids=["fp32", "bf16"])
-@pytest.mark.parametrize("shape", [3, 5, 10, 11])
+@pytest.mark.parametrize("shape", [3, 5, 10, 11, 12, 13])
 def test_rows_that_see_nothing_get_zeros(shape, fp32):
     rows, lens, hq, hkv, hd = ATT_SHAPES[shape]
     c = Case(rows, lens, hq, hkv, hd, torch.float32 if fp32 else torch.bfloat16, seed=5, junk=math.inf)
@@ -358,7 +361,7 @@ def test_rows_that_see_nothing_get_zeros(shape, fp32):
 
 @pytest.mark.parametrize("bits", [math.nan, math.inf, -math.inf, torch.finfo(torch.bfloat16).min], ids=str)
 @pytest.mark.parametrize("fp32", [True, False], ids=["fp32", "bf16"])
-@pytest.mark.parametrize("shape", [0, 3, 4, 8, 10, 11])
+@pytest.mark.parametrize("shape", [0, 3, 4, 8, 10, 11, 12, 13])
 def test_what_a_row_does_not_see_does_not_reach_it(shape, fp32, bits):
     """Keys and values of another document of the same sequence, of later positions and of slots past the end hold `bits`:
     rows that do not see them are, bit for bit, what they are without."""
@@ -392,7 +395,7 @@ def test_what_a_row_does_not_see_does_not_reach_it(shape, fp32, bits):
         assert not torch.isfinite(got[sick].view(-1, hq, hd)[:, :, 5]).any()
 
 
-@pytest.mark.parametrize("shape", [4, 10])
+@pytest.mark.parametrize("shape", [4, 10, 12])
 def test_large_and_equal_scores(shape):
     """Scores near the top of the float range, and rows whose scores are all alike."""
     rows, lens, hq, hkv, hd = ATT_SHAPES[shape]
@@ -427,7 +430,7 @@ def test_attention_pages_outside_the_pool_read_as_zeros():
 
 
 @pytest.mark.parametrize("fp32", [True, False], ids=["fp32", "bf16"])
-@pytest.mark.parametrize("shape", [2, 4, 10])
+@pytest.mark.parametrize("shape", [2, 4, 10, 12, 13])
 def test_attention_in_place(shape, fp32):
     rows, lens, hq, hkv, hd = ATT_SHAPES[shape]
     c = Case(rows, lens, hq, hkv, hd, torch.float32 if fp32 else torch.bfloat16, seed=6)
@@ -492,7 +495,7 @@ def test_offsets_past_32_bits():
     assert torch.equal(pool[:, :, n_pages - 4], src)
 
 
-@pytest.mark.parametrize("shape", [2, 5, 6, 10])
+@pytest.mark.parametrize("shape", [2, 5, 6, 10, 13])
 def test_attention_captured_and_replayed(shape):
     """Captured with one batch, replayed while lengths and keys change in place; eager calls in between."""
     rows, lens, hq, hkv, hd = ATT_SHAPES[shape]
