@@ -11,33 +11,32 @@ __device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? l
 // The newest rows of a sequence and where they stand.
 struct SeqRows { int b, r0, n, len; };   // sequence (-1: none), first row, rows, keys
 
-// Sequence of item t where sequence b owns the items first(b) .. first(b + 1) - 1 of an ascending `first`: the last b
-// with first(b) <= t, by a search 64 ways wide (one load a lane and step).  All lanes of the wave are active, t is uniform.
-template <typename First>
-__device__ __forceinline__ int find_seq(int n_seq, First first, int t) {
-    const int lane = threadIdx.x & 63;
-    int lo = 0, n = n_seq;   // the answer is lo - 1 .. lo + n - 1 (lo - 1 only while lo is 0)
-    while (n > 0) {
-        const int step = (n + 63) / 64, b = lo + lane * step;
-        const int c = __popcll(__builtin_amdgcn_ballot_w64(b < lo + n && first(b) <= t));
-        if (c == 0) return lo - 1;
-        const int end = lo + n;
-        lo += (c - 1) * step;
-        if (step == 1) return lo;
-        n = (lo + step < end ? lo + step : end) - lo;
-    }
-    return -1;
-}
-
 __device__ __forceinline__ int row_at(const PagedKv& kv, int b) { return clampi(kv.row_start[b], 0, kv.n_rows); }
 
-__device__ __forceinline__ SeqRows seq_rows(const PagedKv& kv, int b) {
-    SeqRows s{b, 0, 0, 0};
-    if (b < 0) return s;
-    s.r0 = row_at(kv, b);
-    s.n = row_at(kv, b + 1) - s.r0;
-    s.len = clampi(kv.kv_len[b], 0, kv.max_len);
-    if (s.n <= 0) s.b = -1;
+// The sequence of item t, where sequence b owns the items first(r0, b) .. of its first row r0 up to the next sequence's: the last b with
+// first(row_start[b], b) <= t, `first` ascending.  64 sequences are looked at at once, a lane each, with all that is asked of them in one
+// trip to memory; more are first searched 64 ways at a time.  All lanes of the wave are active, t is uniform.
+template <typename First>
+__device__ __forceinline__ SeqRows find_rows(const PagedKv& kv, First first, int t) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = kv.n_seq;   // the answer is lo .. lo + n - 1 (or none, while lo is 0)
+    while (n > 64) {
+        const int step = (n + 63) / 64, b = lo + lane * step;
+        const int c = __popcll(__builtin_amdgcn_ballot_w64(b < lo + n && first(row_at(kv, b < lo + n ? b : lo), b) <= t));
+        if (c == 0) return SeqRows{-1, 0, 0, 0};
+        const int end = lo + n;
+        lo += (c - 1) * step;
+        n = (lo + step < end ? lo + step : end) - lo;
+    }
+    const int b = lo + (lane < n ? lane : 0);
+    const int r0 = row_at(kv, b), r1 = row_at(kv, b + 1), len = clampi(kv.kv_len[b], 0, kv.max_len);
+    const int c = __popcll(__builtin_amdgcn_ballot_w64(lane < n && first(r0, b) <= t));
+    SeqRows s{-1, 0, 0, 0};
+    if (c == 0) return s;
+    s.r0 = __builtin_amdgcn_readlane(r0, c - 1);
+    s.n = __builtin_amdgcn_readlane(r1, c - 1) - s.r0;
+    s.len = __builtin_amdgcn_readlane(len, c - 1);
+    s.b = s.n > 0 ? lo + c - 1 : -1;
     return s;
 }
 
@@ -82,12 +81,10 @@ template <int HD, typename XT>
 __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a, int qk_slices) {
     const int tid = threadIdx.x, Hq = a.n_heads, Hkv = a.kv.n_kv_heads, rot = a.rot_dim, half = rot / 2;
     const int t = blockIdx.x;
-    const auto first = [&](int b) { return row_at(a.kv, b) / SB_KV_BLOCK + 2 * b; };
-    const int b = __builtin_amdgcn_readfirstlane(find_seq(a.kv.n_seq, first, t));
-    const SeqRows s = seq_rows(a.kv, b);
+    const SeqRows s = find_rows(a.kv, [](int r0, int b) { return r0 / SB_KV_BLOCK + 2 * b; }, t);
     if (s.b < 0) return;
     const int pos0 = s.len - s.n, from = pos0 > 0 ? pos0 : 0;
-    const int page = from / SB_KV_BLOCK + t - (s.r0 / SB_KV_BLOCK + 2 * b);
+    const int page = from / SB_KV_BLOCK + t - (s.r0 / SB_KV_BLOCK + 2 * s.b);
     const int lo = page * SB_KV_BLOCK > from ? page * SB_KV_BLOCK : from;
     int hi = (page + 1) * SB_KV_BLOCK < s.len ? (page + 1) * SB_KV_BLOCK : s.len;
     if (rot && hi > a.n_pos) hi = a.n_pos;
@@ -246,12 +243,10 @@ __device__ __forceinline__ int half_max(int v) { return -half_min(-v); }
 template <int TQ>
 __device__ __forceinline__ SeqRows tile_seq(const PagedAttnArgs& a, int t, int& q0) {
     const int G = a.group;
-    const auto first = [&](int b) { return row_at(a.kv, b) * G / TQ + b; };
-    const int b = __builtin_amdgcn_readfirstlane(find_seq(a.kv.n_seq, first, t));
-    SeqRows s = seq_rows(a.kv, b);
+    SeqRows s = find_rows(a.kv, [G](int r0, int b) { return r0 * G / TQ + b; }, t);
     q0 = 0;
     if (s.b >= 0) {
-        q0 = (t - (s.r0 * G / TQ + b)) * TQ;
+        q0 = (t - (s.r0 * G / TQ + s.b)) * TQ;
         if (q0 >= s.n * G) s.b = -1;
     }
     return s;
@@ -318,38 +313,53 @@ __device__ __forceinline__ Steps steps_of(const Reach& w) {
     return t;
 }
 
-// A row's values as PARTS bf16 B operands: one for bf16 rows, three for float rows (8 + 8 + 8 bits: all of them).
+// Eight values as PARTS bf16 B operands: one for bf16 rows, three for float rows (8 + 8 + 8 bits: all of them).
+template <int PARTS>
+__device__ __forceinline__ void split8(const void* rows, int64_t at, bf16x8 (&op)[PARTS]) {
+    if constexpr (PARTS == 1) {
+        op[0] = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const uint16_t*>(rows) + at);
+    } else {
+        const float* p = reinterpret_cast<const float*>(rows) + at;
+        const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
+        float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                w[e] = pack_bf16(f[2 * e], f[2 * e + 1]);
+                f[2 * e] -= __uint_as_float(w[e] << 16);
+                f[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+            }
+            op[i] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+        }
+    }
+}
 template <int HD, int PARTS>
 __device__ __forceinline__ void load_query(const PagedAttnArgs& a, const Query& q, int lh, bf16x8 (&op)[PARTS][HD / 16]) {
-    const int64_t at = (int64_t)q.row * a.ld_q + q.head * HD + lh * 8;
-    if constexpr (PARTS == 1) {
-        const uint16_t* p = reinterpret_cast<const uint16_t*>(a.q) + at;
 #pragma unroll
-        for (int ks = 0; ks < HD / 16; ++ks) op[0][ks] = *reinterpret_cast<const bf16x8*>(p + ks * 16);
-    } else {
-        const float* p = reinterpret_cast<const float*>(a.q) + at;
+    for (int ks = 0; ks < HD / 16; ++ks) {
+        bf16x8 t[PARTS];
+        split8<PARTS>(a.q, (int64_t)q.row * a.ld_q + q.head * HD + lh * 8 + ks * 16, t);
 #pragma unroll
-        for (int ks = 0; ks < HD / 16; ++ks) {
-            const float4 x = *reinterpret_cast<const float4*>(p + ks * 16), y = *reinterpret_cast<const float4*>(p + ks * 16 + 4);
-            float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-#pragma unroll
-            for (int i = 0; i < PARTS; ++i) {
-                uint32_t w[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    w[e] = pack_bf16(f[2 * e], f[2 * e + 1]);
-                    f[2 * e] -= __uint_as_float(w[e] << 16);
-                    f[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
-                }
-                op[i][ks] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-            }
-        }
+        for (int i = 0; i < PARTS; ++i) op[i][ks] = t[i];
     }
 }
 
 // Register r of a key tile's scores in lane (li, lh): query li, key key0 + 16 (r / 8) + 8 lh + r % 8.
 __device__ __forceinline__ int reg_key(int r) { return (r >> 3) * 16 + (r & 7); }
 
+// tanh x to a few units in the last place: its series up to x^11 below 0.3 (the next term is 2e-9 of x there), 1 - 2 / (exp 2x + 1) above.
+__device__ __forceinline__ float tanh_near(float x) {
+    const float y = x * x;
+    float t = fmaf(y, -8.8632355e-3f, 2.1869488e-2f);
+    t = fmaf(y, t, -5.3968254e-2f);
+    t = fmaf(y, t, 0.13333333f);
+    t = fmaf(y, t, -0.33333333f);
+    t = fmaf(x * y, t, x);
+    const float e = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(fabsf(x) * (2.f * LOG2E)) + 1.f), 1.f);
+    return y < 0.09f ? t : copysignf(e, x);
+}
 // Cap and bias, where there are any: scores in units of log 2 then, raw products else.
 template <int PARTS, int KT, bool SHAPED>
 __device__ __forceinline__ void shape_scores(const PagedAttnArgs& a, const Query& q, int key0, int lh, f32x16 (&st)[KT]) {
@@ -368,7 +378,7 @@ __device__ __forceinline__ void shape_scores(const PagedAttnArgs& a, const Query
 #pragma unroll
             for (int t = 0; t < KT; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) st[t][r] = c2 * tanhf(st[t][r] * k);
+                for (int r = 0; r < 16; ++r) st[t][r] = c2 * tanh_near(st[t][r] * k);
         }
     } else if (a.slopes) {
         const float c2 = a.scale * LOG2E;
@@ -518,7 +528,7 @@ struct Partials {
 // turn with a running soft-max each, operands straight from the cache into registers, the next step's keys requested when
 // this step's scores are done and its values when its products are; the waves' results are added in wave order through LDS.
 template <int HD, int PARTS>
-__global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void paged_attn_apart_kernel(PagedAttnArgs a, int steps_per_chunk) {
+__global__ __launch_bounds__(256, 2) void paged_attn_apart_kernel(PagedAttnArgs a, int steps_per_chunk) {
     constexpr int W = 4, KS = HD / 16, DT = HD / 32, SLAB = SB_KV_BLOCK * HD, NS = DT * 4;
     __shared__ __attribute__((aligned(16))) float o_s[W][NS][64][4];
     __shared__ float m_s[W][32], l_s[W][32];
@@ -579,8 +589,30 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void paged_attn_apart_kern
         cp0 = pg0; cp1 = pg1;
         if (i + W < last) lookup(i + W);
     }
-    bf16x8 qo[PARTS][KS];
-    load_query<HD, PARTS>(a, q, lh, qo);
+    // The queries: bf16 rows in registers; the three parts of float rows in LDS, made once for the four waves (in registers they would leave
+    // one block per CU), where the results go later.
+    bf16x8 qo[KS];
+    bf16x8* const q_s = reinterpret_cast<bf16x8*>(&o_s[0][0][0][0]);   // [PARTS][KS][64 lanes]
+    static_assert(PARTS * KS * 64 * 16 <= (int)sizeof(o_s), "the queries fit where the results go");
+    if constexpr (PARTS == 1) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            bf16x8 t[1];
+            split8<1>(a.q, (int64_t)q.row * a.ld_q + q.head * HD + lh * 8 + ks * 16, t);
+            qo[ks] = t[0];
+        }
+    } else {
+        const int x = tid / 8, qq = q0 + x < s.n * a.group ? q0 + x : q0, r = qq / a.group;   // (past the end: the first one, not stored)
+        const int64_t at = (int64_t)(s.r0 + r) * a.ld_q + (g * a.group + qq - r * a.group) * HD;
+#pragma unroll
+        for (int y = tid % 8; y < HD / 8; y += 8) {
+            bf16x8 t[PARTS];
+            split8<PARTS>(a.q, at + y * 8, t);
+#pragma unroll
+            for (int z = 0; z < PARTS; ++z) q_s[(z * KS + y / 2) * 64 + (y & 1) * 32 + x] = t[z];
+        }
+        __syncthreads();
+    }
     const float mul = score_mul(a);
     f32x16 o[DT];
     float m_run = -SB_INF, l_run = 0.f;
@@ -605,9 +637,14 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void paged_attn_apart_kern
 #pragma unroll
         for (int r = 0; r < 16; ++r) st[0][r] = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
+        for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
-            for (int x = 0; x < PARTS; ++x) st[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[ks]), qo[x][ks], st[0], 0, 0, 0);
+            for (int x = 0; x < PARTS; ++x) {
+                const bf16x8 qx = PARTS == 1 ? qo[ks] : q_s[(x * KS + ks) * 64 + lane];
+                st[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[ks]), qx, st[0], 0, 0, 0);
+            }
+            if (PARTS > 1 && ks % 2) __builtin_amdgcn_sched_barrier(0);   // (six operands from LDS at a time: registers)
+        }
         const bool more = i + W < last;
         const int np0 = pg0, np1 = pg1;
         if (more) {
@@ -706,7 +743,7 @@ __global__ __launch_bounds__(256) void paged_attn_merge_kernel(PagedAttnArgs a, 
     __shared__ float ls[NG];
     __shared__ __attribute__((aligned(16))) float os[NG][HD];
     const int tid = threadIdx.x, row = blockIdx.x / a.n_heads, head = blockIdx.x % a.n_heads, grp = tid / L, d = tid % L * 4;
-    const SeqRows s = seq_rows(a.kv, __builtin_amdgcn_readfirstlane(find_seq(a.kv.n_seq, [&](int b) { return row_at(a.kv, b); }, row)));
+    const SeqRows s = find_rows(a.kv, [](int r0, int) { return r0; }, row);
     if (s.b < 0 || row >= s.r0 + s.n) return;
     const Partials part(a.scratch, (int64_t)a.kv.n_rows * a.n_heads, chunks, HD);
     const int64_t pair = blockIdx.x, at = pair * chunks;
@@ -960,9 +997,8 @@ static AttnPlan attn_plan(const PagedKv& kv, int32_t n_heads) {
         return p;
     }
     p.tiles = kv.n_rows * G / 32 + kv.n_seq;
-    const int64_t want = (p.tiles * kv.n_kv_heads * total + 2047) / 2048;
+    const int64_t want = (p.tiles * kv.n_kv_heads * total + 511) / 512;
     p.steps = (int)(want < 4 ? 4 : want > 64 ? 64 : (want + 3) / 4 * 4);
-    if (p.tiles * kv.n_kv_heads >= 1024) p.steps = (int)((total + 3) / 4 * 4);
     if (total / p.steps > 512) p.steps = (int)((total / 512 + 3) / 4 * 4);
     p.chunks = (int)((total + p.steps - 1) / p.steps);
     return p;
