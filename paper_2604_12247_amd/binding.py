@@ -662,24 +662,24 @@ def _dtype_code(t):
     raise TypeError(f"expected float32 or bfloat16 rows, not {t.dtype}")
 
 
-def _need(t, name, device, dtype=None, ndim=None):
-    """A tensor argument on the GPU of the pool; its pointer (None stays None)."""
+def _vector(t, name, n, dtype, index):
+    """Pointer of a dense vector argument on GPU `index` (None stays None)."""
     if t is None:
         return None
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the pool on {device}")
-    if dtype is not None and t.dtype != dtype:
+    if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if ndim is not None and (t.dim() != ndim or not t.is_contiguous()):
-        raise ValueError(f"{name} must be contiguous with {ndim} dimension(s), not {tuple(t.shape)}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, the pool on cuda:{index}")
+    if t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be {n} neighbouring elements, not {tuple(t.shape)} of strides {t.stride()}")
     return t.data_ptr()
 
 
-def _rows(t, name, n_rows, width, device):
+def _rows(t, name, n_rows, width, index):
     """Rows of a 2-d operand: its pointer, the elements from one row to the next."""
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the pool on {device}")
-    if t.dim() != 2 or t.shape[0] != n_rows or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, the pool on cuda:{index}")
+    if t.shape != (n_rows, width) or t.stride(1) != 1:
         raise ValueError(f"{name} must be [{n_rows}, {width}] with rows of neighbouring elements, not {tuple(t.shape)} of strides {t.stride()}")
     return t.data_ptr(), t.stride(0) if n_rows > 1 else width
 
@@ -709,30 +709,33 @@ class Paged:
             raise TypeError(f"table must be torch.int32, not {table.dtype}")
         if table.device != dev:
             raise ValueError(f"table is on {table.device}, the pool on {dev}")
-        _need(row_start, "row_start", dev, torch.int32, 1)
-        _need(kv_len, "kv_len", dev, torch.int32, 1)
-        if row_start.shape[0] != n_seq + 1 or kv_len.shape[0] != n_seq:
-            raise ValueError(f"{n_seq} sequences need row_start [{n_seq + 1}] and kv_len [{n_seq}], not {tuple(row_start.shape)} and {tuple(kv_len.shape)}")
+        index = pool.get_device()
+        row_ptr = _vector(row_start, "row_start", n_seq + 1, torch.int32, index)
+        len_ptr = _vector(kv_len, "kv_len", n_seq, torch.int32, index)
         cap = SB_KV_BLOCK * table.shape[1]
         max_len = cap if max_len is None else int(max_len)
         if not 1 <= max_len <= cap:
             raise ValueError(f"max_len must be in 1..{cap}, not {max_len}")
         self.pool, self.table, self.row_start, self.kv_len = pool, table, row_start, kv_len
-        self.device, self.n_rows = dev, int(n_rows)
+        self.torch, self.device, self.index, self.n_rows = torch, dev, index, int(n_rows)
         self.n_layers, _, self.n_pages, self.n_kv_heads, _, self.head_dim = pool.shape
         ld = table.stride(0) if n_seq > 1 else table.shape[1]
-        self.c = sb_paged(pool.data_ptr(), table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(), self.n_pages, self.n_kv_heads,
-                          self.head_dim, n_seq, self.n_rows, ld, max_len)
+        self.n_seq = n_seq
+        self.c = sb_paged(pool.data_ptr(), table.data_ptr(), row_ptr, len_ptr, self.n_pages, self.n_kv_heads, self.head_dim, n_seq, self.n_rows,
+                          ld, max_len)
+        self.ref = C.byref(self.c)
 
     def _call(self, layer, fn, *args):
-        import torch
         if not 0 <= layer < self.n_layers:
             raise ValueError(f"layer must be in 0..{self.n_layers - 1}, not {layer}")
-        st = torch._C._cuda_getCurrentRawStream(self.device.index)
-        if torch.cuda.current_device() == self.device.index:
-            return check(fn(C.byref(self.c), layer, *args, st))
-        with torch.cuda.device(self.device):
-            check(fn(C.byref(self.c), layer, *args, st))
+        c = self.torch._C
+        if c._cuda_getDevice() == self.index:
+            rc = fn(self.ref, layer, *args, c._cuda_getCurrentRawStream(self.index))
+        else:
+            with self.torch.cuda.device(self.device):
+                rc = fn(self.ref, layer, *args, c._cuda_getCurrentRawStream(self.index))
+        if rc:
+            check(rc)
 
 
 def op_rope_append(kv: Paged, qkv, n_heads: int, rope_cos, rope_sin, interleaved: bool = False, q_gain=None, k_gain=None,
@@ -743,26 +746,28 @@ def op_rope_append(kv: Paged, qkv, n_heads: int, rope_cos, rope_sin, interleaved
     qkv [n_rows, (n_heads + 2 n_kv_heads) head_dim] float32 or bfloat16; rope_cos, rope_sin [n_pos, rot_dim / 2] float32
     (rot_dim dims of a head are rotated, the others passed); gains [head_dim] float32.  `out` may be a tensor for the
     result, or the first n_heads * head_dim columns of qkv themselves."""
-    import torch
-    hd, dev = kv.head_dim, kv.device
+    torch, hd, index = kv.torch, kv.head_dim, kv.index
     w = n_heads * hd
-    x, ld = _rows(qkv, "qkv", kv.n_rows, (n_heads + 2 * kv.n_kv_heads) * hd, dev)
+    x, ld = _rows(qkv, "qkv", kv.n_rows, w + 2 * kv.n_kv_heads * hd, index)
     code = _dtype_code(qkv)
-    if rope_cos.shape != rope_sin.shape:
-        raise ValueError(f"rope tables of {tuple(rope_cos.shape)} and {tuple(rope_sin.shape)}")
-    cp, sp = _need(rope_cos, "rope_cos", dev, torch.float32, 2), _need(rope_sin, "rope_sin", dev, torch.float32, 2)
-    qg, kg = _need(q_gain, "q_gain", dev, torch.float32, 1), _need(k_gain, "k_gain", dev, torch.float32, 1)
-    for g in (q_gain, k_gain):
-        if g is not None and g.shape[0] != hd:
-            raise ValueError(f"a gain of {g.shape[0]} for heads of {hd}")
+    if rope_cos.dim() != 2 or rope_cos.shape != rope_sin.shape or not rope_cos.is_contiguous() or not rope_sin.is_contiguous():
+        raise ValueError(f"rope tables must be contiguous [n_pos, rot_dim / 2], not {tuple(rope_cos.shape)} and {tuple(rope_sin.shape)}")
+    if rope_cos.dtype != torch.float32 or rope_sin.dtype != torch.float32:
+        raise TypeError(f"rope tables must be float32, not {rope_cos.dtype} and {rope_sin.dtype}")
+    if rope_cos.get_device() != index or rope_sin.get_device() != index:
+        raise ValueError(f"rope tables are on {rope_cos.device} and {rope_sin.device}, the pool on cuda:{index}")
+    qg, kg = _vector(q_gain, "q_gain", hd, torch.float32, index), _vector(k_gain, "k_gain", hd, torch.float32, index)
     if out is None:
-        out = torch.empty((kv.n_rows, w), dtype=qkv.dtype, device=dev)
-    elif out.dtype != qkv.dtype:
-        raise TypeError(f"out must be {qkv.dtype}, not {out.dtype}")
-    o, ldo = _rows(out, "out", kv.n_rows, w, dev)
-    if kv.n_rows == 1 and o == x:
-        ldo = ld
-    kv._call(layer, lib().sb_op_rope_append, x, code, ld, n_heads, qg, kg, eps, cp, sp, rope_cos.shape[0], 2 * rope_cos.shape[1],
+        out = torch.empty((kv.n_rows, w), dtype=qkv.dtype, device=kv.device)
+        o, ldo = out.data_ptr(), w
+    else:
+        if out.dtype != qkv.dtype:
+            raise TypeError(f"out must be {qkv.dtype}, not {out.dtype}")
+        o, ldo = _rows(out, "out", kv.n_rows, w, index)
+        if kv.n_rows == 1 and o == x:
+            ldo = ld
+    n_pos, half = rope_cos.shape
+    kv._call(layer, lib().sb_op_rope_append, x, code, ld, n_heads, qg, kg, eps, rope_cos.data_ptr(), rope_sin.data_ptr(), n_pos, 2 * half,
              ROPE_INTERLEAVED if interleaved else ROPE_HALF, o, ldo)
     return out
 
@@ -770,7 +775,7 @@ def op_rope_append(kv: Paged, qkv, n_heads: int, rope_cos, rope_sin, interleaved
 def paged_attention_scratch(kv: Paged, n_heads: int):
     """A scratch area for op_paged_attention calls on kv (calls that may overlap need one each)."""
     import torch
-    n = lib().sb_op_paged_attention_scratch_bytes(C.byref(kv.c), n_heads)
+    n = lib().sb_op_paged_attention_scratch_bytes(kv.ref, n_heads)
     return torch.empty(max(n, 256), dtype=torch.uint8, device=kv.device)
 
 
@@ -782,29 +787,29 @@ def op_paged_attention(kv: Paged, q, n_heads: int, scale: float = 0.0, softcap: 
     A row at position p sees key k of its sequence if k >= doc_start[row] and (k < prefix_len[sequence], or k <= p and, with
     a window, k > p - window).  Scores: scale q.k (0: 1 / sqrt(head_dim)), softcap * tanh(. / softcap) where softcap > 0,
     less slopes[head] * |p - k|.  slopes [n_heads] float32, prefix_len [n_seq] and doc_start [n_rows] int32."""
-    import torch
-    dev = kv.device
+    torch, index = kv.torch, kv.index
     w = n_heads * kv.head_dim
-    x, ld = _rows(q, "q", kv.n_rows, w, dev)
+    x, ld = _rows(q, "q", kv.n_rows, w, index)
     code = _dtype_code(q)
-    rule = sb_attn_rule(scale, softcap, _need(slopes, "slopes", dev, torch.float32, 1), window,
-                        _need(prefix_len, "prefix_len", dev, torch.int32, 1), _need(doc_start, "doc_start", dev, torch.int32, 1))
-    for t, name, n in ((slopes, "slopes", n_heads), (prefix_len, "prefix_len", kv.c.n_seq), (doc_start, "doc_start", kv.n_rows)):
-        if t is not None and t.shape[0] != n:
-            raise ValueError(f"{name} must have {n} entries, not {t.shape[0]}")
+    rule = None
+    if scale or softcap or window or slopes is not None or prefix_len is not None or doc_start is not None:
+        rule = C.byref(sb_attn_rule(scale, softcap, _vector(slopes, "slopes", n_heads, torch.float32, index), window,
+                                    _vector(prefix_len, "prefix_len", kv.n_seq, torch.int32, index),
+                                    _vector(doc_start, "doc_start", kv.n_rows, torch.int32, index)))
     if out is None:
-        out = torch.empty((kv.n_rows, w), dtype=q.dtype, device=dev)
-    elif out.dtype != q.dtype:
-        raise TypeError(f"out must be {q.dtype}, not {out.dtype}")
-    o, ldo = _rows(out, "out", kv.n_rows, w, dev)
-    if kv.n_rows == 1 and o == x:
-        ldo = ld
+        out = torch.empty((kv.n_rows, w), dtype=q.dtype, device=kv.device)
+        o, ldo = out.data_ptr(), w
+    else:
+        if out.dtype != q.dtype:
+            raise TypeError(f"out must be {q.dtype}, not {out.dtype}")
+        o, ldo = _rows(out, "out", kv.n_rows, w, index)
+        if kv.n_rows == 1 and o == x:
+            ldo = ld
     if scratch is None:
         scratch = paged_attention_scratch(kv, n_heads)
-    elif scratch.device != dev or not scratch.is_contiguous():
-        raise ValueError(f"scratch must be contiguous on {dev}")
-    kv._call(layer, lib().sb_op_paged_attention, x, code, ld, n_heads, C.byref(rule), o, ldo, scratch.data_ptr(),
-             scratch.numel() * scratch.element_size())
+    elif scratch.get_device() != index or not scratch.is_contiguous():
+        raise ValueError(f"scratch must be contiguous on cuda:{index}")
+    kv._call(layer, lib().sb_op_paged_attention, x, code, ld, n_heads, rule, o, ldo, scratch.data_ptr(), scratch.nbytes)
     return out
 
 
@@ -820,10 +825,14 @@ def op_copy_pages(dst, src, dst_pages: Sequence[int], src_pages: Sequence[int]):
     d, s = (np.ascontiguousarray(p, dtype=np.int32) for p in (dst_pages, src_pages))
     if d.ndim != 1 or d.shape != s.shape:
         raise ValueError("dst_pages and src_pages must be lists of one length")
-    page_bytes = src[0, 0, 0].numel() * src.element_size()
-    with torch.cuda.device(src.device):
-        check(lib().sb_op_copy_pages(dst.data_ptr(), dst.shape[2], src.data_ptr(), src.shape[2], page_bytes, 2 * src.shape[0], d.ctypes.data,
-                                     s.ctypes.data, len(d), _stream_ptr(torch, src)))
+    page_bytes, index = src.stride(2) * src.element_size(), src.get_device()
+    args = (dst.data_ptr(), dst.shape[2], src.data_ptr(), src.shape[2], page_bytes, 2 * src.shape[0], d.ctypes.data, s.ctypes.data, len(d),
+            torch._C._cuda_getCurrentRawStream(index))
+    if torch._C._cuda_getDevice() == index:
+        check(lib().sb_op_copy_pages(*args))
+    else:
+        with torch.cuda.device(index):
+            check(lib().sb_op_copy_pages(*args))
 
 
 class Pages:

@@ -75,10 +75,11 @@ __device__ __forceinline__ uint32_t load_pair(const uint16_t* p) { return *reint
 // the lane but for the sum of squares; ROPE_U heads a thread in flight.
 //   v: a thread takes two dims and eight slots, and its page half leaves as 16-byte pieces of the transposed slab where all
 // eight are new.
-constexpr int ROPE_QK = 16, ROPE_V = 8, ROPE_U = 4;
+constexpr int ROPE_U = 4;
 
 template <int HD, typename XT>
-__global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a, int qk_slices) {
+__global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a, int qk_heads, int qk_slices) {
+    constexpr int ROPE_V = 256 / HD;   // v heads of a block: one item a thread
     const int tid = threadIdx.x, Hq = a.n_heads, Hkv = a.kv.n_kv_heads, rot = a.rot_dim, half = rot / 2;
     const int t = blockIdx.x;
     const SeqRows s = find_rows(a.kv, [](int r0, int b) { return r0 / SB_KV_BLOCK + 2 * b; }, t);
@@ -97,8 +98,8 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a, int 
 
     if ((int)blockIdx.y < qk_slices) {
         constexpr int L = HD / 8, SIDE = 256 / L;
-        const int c = tid % L, h0 = blockIdx.y * ROPE_QK;
-        const int nh = Hq + Hkv - h0 < ROPE_QK ? Hq + Hkv - h0 : ROPE_QK, n = nr * nh;
+        const int c = tid % L, h0 = blockIdx.y * qk_heads;
+        const int nh = Hq + Hkv - h0 < qk_heads ? Hq + Hkv - h0 : qk_heads, n = nr * nh;
         const bool turns = c < rot / 8;
         const int dA = a.interleaved ? 8 * c : turns ? 4 * c : rot + 8 * (c - rot / 8);
         const int dB = a.interleaved || !turns ? dA + 4 : dA + half;
@@ -168,45 +169,45 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a, int 
         return;
     }
     if (!in_pool) return;
-    const int g0 = (blockIdx.y - qk_slices) * ROPE_V, ng = Hkv - g0 < ROPE_V ? Hkv - g0 : ROPE_V;
+    const int g = (blockIdx.y - qk_slices) * ROPE_V + tid / HD, d = tid % HD & ~1, t0 = (tid & 1) * 8;
     const int s_lo = lo % SB_KV_BLOCK, s_hi = s_lo + nr;   // new slots of the page
-    for (int i = tid; i < ng * HD; i += 256) {
-        const int g = g0 + i / HD, d = i % HD & ~1, t0 = (i & 1) * 8;
-        if (t0 >= s_hi || t0 + 8 <= s_lo) continue;
-        const XT* p = x + (Hq + Hkv + g) * HD + d;
-        uint32_t w[8];
+    if (g >= Hkv || t0 >= s_hi || t0 + 8 <= s_lo) return;
+    const XT* p = x + (Hq + Hkv + g) * HD + d;
+    uint32_t w[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {   // (no condition, so the eight go out together)
-            const int sl = t0 + e < s_lo ? s_lo : t0 + e < s_hi ? t0 + e : s_hi - 1;
-            w[e] = load_pair(p + (row0 + sl - s_lo) * a.ld_qkv);
+    for (int e = 0; e < 8; ++e) {   // (no condition, so the eight go out together)
+        const int sl = t0 + e < s_lo ? s_lo : t0 + e < s_hi ? t0 + e : s_hi - 1;
+        w[e] = load_pair(p + (row0 + sl - s_lo) * a.ld_qkv);
+    }
+    uint16_t* dst = a.kv.v + slab + (g * HD + d) * SB_KV_BLOCK + t0;
+    if (t0 >= s_lo && t0 + 8 <= s_hi) {
+        uint32_t lo2[4], hi2[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            lo2[e] = (w[2 * e] & 0xffffu) | (w[2 * e + 1] << 16);
+            hi2[e] = (w[2 * e] >> 16) | (w[2 * e + 1] & 0xffff0000u);
         }
-        uint16_t* dst = a.kv.v + slab + (g * HD + d) * SB_KV_BLOCK + t0;
-        if (t0 >= s_lo && t0 + 8 <= s_hi) {
-            uint32_t lo2[4], hi2[4];
+        *reinterpret_cast<uint4*>(dst) = make_uint4(lo2[0], lo2[1], lo2[2], lo2[3]);
+        *reinterpret_cast<uint4*>(dst + SB_KV_BLOCK) = make_uint4(hi2[0], hi2[1], hi2[2], hi2[3]);
+    } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                lo2[e] = (w[2 * e] & 0xffffu) | (w[2 * e + 1] << 16);
-                hi2[e] = (w[2 * e] >> 16) | (w[2 * e + 1] & 0xffff0000u);
+        for (int e = 0; e < 8; ++e)
+            if (t0 + e >= s_lo && t0 + e < s_hi) {
+                dst[e] = (uint16_t)w[e];
+                dst[SB_KV_BLOCK + e] = (uint16_t)(w[e] >> 16);
             }
-            *reinterpret_cast<uint4*>(dst) = make_uint4(lo2[0], lo2[1], lo2[2], lo2[3]);
-            *reinterpret_cast<uint4*>(dst + SB_KV_BLOCK) = make_uint4(hi2[0], hi2[1], hi2[2], hi2[3]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (t0 + e >= s_lo && t0 + e < s_hi) {
-                    dst[e] = (uint16_t)w[e];
-                    dst[SB_KV_BLOCK + e] = (uint16_t)(w[e] >> 16);
-                }
-        }
     }
 }
 
 hipError_t launch_rope_append(const RopeAppendArgs& a, hipStream_t st) {
-    const int qk = (a.n_heads + a.kv.n_kv_heads + ROPE_QK - 1) / ROPE_QK, v = (a.kv.n_kv_heads + ROPE_V - 1) / ROPE_V;
+    // q and k heads of a block: about ROPE_U a thread (16 threads a head of 128) for as many rows as a page gets on average.
+    const int64_t rows = a.kv.n_rows / a.kv.n_seq;
+    const int qk_heads = rows >= 8 ? 4 : rows >= 3 ? 8 : 16, v_heads = 256 / a.kv.head_dim;
+    const int qk = (a.n_heads + a.kv.n_kv_heads + qk_heads - 1) / qk_heads, v = (a.kv.n_kv_heads + v_heads - 1) / v_heads;
     const dim3 grid(a.kv.n_rows / SB_KV_BLOCK + 2 * a.kv.n_seq, qk + v);
     const auto go = [&](auto hd_c) {
         constexpr int HD = decltype(hd_c)::value;
-        return launch(a.x_dtype == SB_FP32 ? &rope_append_kernel<HD, float> : &rope_append_kernel<HD, uint16_t>, grid, 256, st, a, qk);
+        return launch(a.x_dtype == SB_FP32 ? &rope_append_kernel<HD, float> : &rope_append_kernel<HD, uint16_t>, grid, 256, st, a, qk_heads, qk);
     };
     return a.kv.head_dim == 128 ? go(std::integral_constant<int, 128>{}) : go(std::integral_constant<int, 64>{});
 }
@@ -349,16 +350,18 @@ __device__ __forceinline__ void load_query(const PagedAttnArgs& a, const Query& 
 // Register r of a key tile's scores in lane (li, lh): query li, key key0 + 16 (r / 8) + 8 lh + r % 8.
 __device__ __forceinline__ int reg_key(int r) { return (r >> 3) * 16 + (r & 7); }
 
-// tanh x to a few units in the last place: its series up to x^11 below 0.3 (the next term is 2e-9 of x there), 1 - 2 / (exp 2x + 1) above.
-__device__ __forceinline__ float tanh_near(float x) {
+// tanh x to a few units in the last place: below 0.3 its series up to x^11 (the next term is 2e-9 of x there), else 1 - 2 / (exp 2x + 1).
+__device__ __forceinline__ float tanh_low(float x) {
     const float y = x * x;
     float t = fmaf(y, -8.8632355e-3f, 2.1869488e-2f);
     t = fmaf(y, t, -5.3968254e-2f);
     t = fmaf(y, t, 0.13333333f);
     t = fmaf(y, t, -0.33333333f);
-    t = fmaf(x * y, t, x);
+    return fmaf(x * y, t, x);
+}
+__device__ __forceinline__ float tanh_near(float x) {
     const float e = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(fabsf(x) * (2.f * LOG2E)) + 1.f), 1.f);
-    return y < 0.09f ? t : copysignf(e, x);
+    return fabsf(x) < 0.3f ? tanh_low(x) : copysignf(e, x);
 }
 // Cap and bias, where there are any: scores in units of log 2 then, raw products else.
 template <int PARTS, int KT, bool SHAPED>
@@ -373,12 +376,21 @@ __device__ __forceinline__ void shape_scores(const PagedAttnArgs& a, const Query
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     st[t][r] = fmaf(-2.f * c2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(st[t][r] * k) + 1.f), c2);
-        } else {
+        } else {   // (mostly all scores of a tile are far below the cap, where the series alone does)
             const float k = a.scale / a.cap;
+            float top = 0.f;
 #pragma unroll
             for (int t = 0; t < KT; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) st[t][r] = c2 * tanh_near(st[t][r] * k);
+                for (int r = 0; r < 16; ++r) {
+                    st[t][r] *= k;
+                    top = __builtin_elementwise_maximum(top, fabsf(st[t][r]));
+                }
+            const bool low = __builtin_amdgcn_ballot_w64(!(top < 0.3f)) == 0;
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st[t][r] = c2 * (low ? tanh_low(st[t][r]) : tanh_near(st[t][r]));
         }
     } else if (a.slopes) {
         const float c2 = a.scale * LOG2E;
@@ -775,39 +787,51 @@ __global__ __launch_bounds__(256) void paged_attn_merge_kernel(PagedAttnArgs a, 
     store_x(a.out, (int64_t)row * a.ld_out + head * HD + tid, a.x_dtype == SB_FP32, t == 0.f ? 0.f : v / t);
 }
 
-// For many rows: a block owns 128 queries of one kv head, 32 a wave, and walks the 64-key steps that any of them sees; the
-// steps' keys and values are staged in LDS for its four waves, two steps deep, by direct global -> LDS loads issued a step ahead (lane l of a
+// For many rows: a block owns 128 queries of one kv head, 32 a wave, and walks the steps of CH keys that any of them sees.  The four waves of a
+// group share a step's keys and values in LDS, two steps deep, by direct global -> LDS loads issued a step ahead (lane l of a
 // wave lands 16 l bytes after the wave's base).  Which piece lands where is chosen so that operand reads are free of bank conflicts: a K piece
 // (key, p) sits at piece p ^ f(key) of its key's row; the two halves (8 keys each) of a V row change places in every second group of 8 dims.
+//   Two waves a SIMD cover for each other: two blocks of one group, or (float rows at head_dim 128, whose three parts would leave one block
+// per CU: the second and third lie in LDS then) one block whose two groups take the steps in turn and add their results at the
+// end.  Such groups are out of step: where one multiplies its keys, the other takes exponentials (group 0 goes keys, soft-max, values;
+// group 1 soft-max, values, the next keys).
+template <int HD, int PARTS>
+struct SharedForm {
+    static constexpr int GROUPS = PARTS > 1 && HD == 128 ? 2 : 1;
+    static constexpr int KT = PARTS == 1 ? 2 : 1;        // 32-key tiles whose scores are held at once
+    static constexpr int CH = GROUPS == 2 ? 32 : 64;     // keys of a step
+};
 template <int HD, int PARTS, bool SHAPED>
-__global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void paged_attn_shared_kernel(PagedAttnArgs a) {
-    constexpr int CH = 64, NT = 256, BQ = 128;
-    constexpr int KT = PARTS == 1 ? 2 : 1;   // 32-key tiles whose scores are held at once
+__global__ __launch_bounds__((256 * SharedForm<HD, PARTS>::GROUPS), 2) void paged_attn_shared_kernel(PagedAttnArgs a) {
+    using F = SharedForm<HD, PARTS>;
+    constexpr int NT = 256, BQ = 128, GROUPS = F::GROUPS, KT = F::KT, CH = F::CH;
+    static_assert(GROUPS == 1 || CH == 32 * KT, "a group that runs ahead holds the scores of a whole step");
     constexpr int KS = HD / 16, DT = HD / 32, PPK = HD / 8, SLAB = SB_KV_BLOCK * HD, NPG = CH / SB_KV_BLOCK;
     constexpr int NL = NPG * SLAB / (NT * 8);   // 16-byte pieces per thread, operand and step
     constexpr int PD = 4;                       // operands are read from LDS PD ahead of their MFMAs
-    __shared__ __attribute__((aligned(16))) uint16_t k_s[2][CH * HD];
-    __shared__ __attribute__((aligned(16))) uint16_t v_s[2][NPG * SLAB];
+    constexpr int NK = KT * KS, NV = 2 * KT * DT, STAGE = CH * HD, IN_LDS = GROUPS == 2 ? PARTS - 1 : 0;   // (parts of the queries)
+    __shared__ __attribute__((aligned(16))) uint16_t kv_s[GROUPS][2][2][STAGE];   // [group][keys, values][turn % 2]
+    __shared__ __attribute__((aligned(16))) bf16x8 q_s[IN_LDS ? IN_LDS * KS * 256 : 1];
+    __shared__ float ml_s[GROUPS][4][32][2];
     __shared__ int reach_s[4][8];
     __shared__ int sick_s;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    static_assert(GROUPS == 1 || sizeof(kv_s) >= 8 * (DT / 2) * 4 * 64 * 16, "the groups' results fit where the steps were");
+    const int lane = threadIdx.x & 63, wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int grp = GROUPS == 2 ? wave8 >> 2 : 0, wave = wave8 & 3, tid = threadIdx.x & 255;
     const int li = lane & 31, lh = lane >> 5;
     const int Hkv = a.kv.n_kv_heads, tiles = gridDim.x / Hkv;
     const int g = blockIdx.x % Hkv;
     int q0;
-    // A prompt's last rows see most: they start first.  Where all blocks are resident at once (two per CU), the second half goes
-    // the other way round, so that a CU's two blocks are a long and a short one.  (The first n_seq are mostly without queries.)
-    const int at = (int)(blockIdx.x / Hkv) - a.kv.n_seq, half = (256 + Hkv - 1) / Hkv, full = tiles - a.kv.n_seq;
-    const SeqRows s = tile_seq<BQ>(a, at >= half && full <= 2 * half ? at - half : full - 1 - at, q0);
+    const SeqRows s = tile_seq<BQ>(a, tiles - 1 - (int)(blockIdx.x / Hkv), q0);   // (a prompt's last rows see most: they start first)
     if (s.b < 0) return;
     Reach w;
     const Query q = lane_query(a, s, g, q0 + wave * 32 + li, w);
-    if (lane == 0) {
+    if (lane == 0 && grp == 0) {
         int* const r = reach_s[wave];
         r[0] = w.a_lo; r[1] = w.b_lo; r[2] = w.a1_min; r[3] = w.b1_min;
         r[4] = w.a_hi; r[5] = w.b_hi; r[6] = w.a0_max; r[7] = w.b0_max;
     }
-    if (tid == 0) sick_s = 0;
+    if (threadIdx.x == 0) sick_s = 0;
     __syncthreads();
     int e8[8];
 #pragma unroll
@@ -819,49 +843,52 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void paged_attn_shared_ker
     }
     const Reach all{e8[0], e8[4], e8[1], e8[5], e8[6], e8[2], e8[7], e8[3]};
     const Steps steps = steps_of<CH>(all);
+    const int turns = (steps.n + GROUPS - 1) / GROUPS;   // of a group; its step in turn j is GROUPS j + grp
 
     const int64_t page_elems = (int64_t)Hkv * SLAB;
     const uint16_t* const kbase = a.kv.k + (int64_t)g * SLAB;
     const uint16_t* const vbase = a.kv.v + (int64_t)g * SLAB;
     const int32_t* const table = a.kv.table + (int64_t)s.b * a.kv.table_ld;
-    // A wave's 64 pieces lie in one page, so the page is a scalar; lane i < NPG of `pg` holds the i-th page of the step
-    // issued next (-1: no key there, or no such page), read one step ahead of the issue.
-    int pg = -1;
-    auto lookup = [&](int i) {
-        const int page = (i < steps.n ? steps.at(i) : 0) * NPG + (lane & (NPG - 1));
-        pg = i < steps.n && page * SB_KV_BLOCK < s.len ? table[page] : -1;
-        if (pg >= a.kv.n_pages) pg = -1;
+    // A wave's 64 pieces lie in one page, so the page is a scalar: lane i < NPG holds the i-th page of a turn's step (-1: no key
+    // there, or no such page: zeros).  A thread's place within a page is the same for all its pieces.
+    auto lookup = [&](int j) {
+        const int i = GROUPS * j + grp, page = (i < steps.n ? steps.at(i) : 0) * NPG + (lane & (NPG - 1));
+        const int pg = i < steps.n && page * SB_KV_BLOCK < s.len ? table[page] : -1;
+        return pg >= a.kv.n_pages ? -1 : pg;
     };
-    // A thread's place within a page is the same for all its pieces: an offset in a register beside a scalar address.
     const int slot_p = (wave * 64 + lane) % (SB_KV_BLOCK * PPK), key_p = slot_p / PPK;
     const uint32_t koff = (uint32_t)(key_p * HD + ((slot_p % PPK) ^ (PPK == 16 ? key_p : (key_p >> 1) & 7)) * 8) * 2;
     const uint32_t voff = (uint32_t)(slot_p ^ ((slot_p >> 4) & 1)) * 16;
-    auto issue = [&](int buf) {
-        uint32_t ko = koff, vo = voff;
-        asm("" : "+v"(ko), "+v"(vo));   // (else base and offset are added outside the loop, and every load adds 64 bits a lane again)
+    auto issue = [&](const uint16_t* base, uint32_t off, uint16_t* lds, int pages) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int slot0 = i * NT + wave * 64;   // the wave's place in LDS
-            const int page = __builtin_amdgcn_readlane(pg, slot0 / (SB_KV_BLOCK * PPK));
-            uint16_t* kw = &k_s[buf][slot0 * 8];
-            uint16_t* vw = &v_s[buf][slot0 * 8];
-            if (page >= 0) {
-                const int64_t base = page * page_elems;
-                __builtin_amdgcn_global_load_lds(reinterpret_cast<const char*>(kbase + base) + ko, kw, 16, 0, 0);
-                __builtin_amdgcn_global_load_lds(reinterpret_cast<const char*>(vbase + base) + vo, vw, 16, 0, 0);
-            } else {
-                *reinterpret_cast<uint4*>(kw + lane * 8) = make_uint4(0, 0, 0, 0);
-                *reinterpret_cast<uint4*>(vw + lane * 8) = make_uint4(0, 0, 0, 0);
-            }
+            const int page = __builtin_amdgcn_readlane(pages, slot0 / (SB_KV_BLOCK * PPK));
+            uint16_t* const at = lds + slot0 * 8;
+            if (page >= 0) __builtin_amdgcn_global_load_lds(reinterpret_cast<const char*>(base + page * page_elems) + off, at, 16, 0, 0);
+            else *reinterpret_cast<uint4*>(at + lane * 8) = make_uint4(0, 0, 0, 0);
         }
     };
-    if (steps.n > 0) {
-        lookup(0);
-        issue(0);
-        lookup(1);
+    int pages_v = lookup(0), pages_k = pages_v;   // of the steps whose values / keys are requested next
+    if (turns > 0) {
+        issue(kbase, koff, kv_s[grp][0][0], pages_k);
+        issue(vbase, voff, kv_s[grp][1][0], pages_v);
+        pages_v = pages_k = lookup(1);
+        if (grp == 1) {   // (its keys are a turn further ahead)
+            issue(kbase, koff, kv_s[grp][0][1], pages_k);
+            pages_k = lookup(2);
+        }
     }
-    bf16x8 qo[PARTS][KS];
-    load_query<HD, PARTS>(a, q, lh, qo);
+    bf16x8 qo[PARTS - IN_LDS][KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        bf16x8 t[PARTS];
+        split8<PARTS>(a.q, (int64_t)q.row * a.ld_q + q.head * HD + lh * 8 + ks * 16, t);
+#pragma unroll
+        for (int x = 0; x < PARTS; ++x)
+            if (x < PARTS - IN_LDS) qo[x][ks] = t[x];
+            else if (grp == 0) q_s[((x - 1) * KS + ks) * 256 + wave * 64 + lane] = t[x];
+    }
     const float mul = score_mul(a);
     f32x16 o[DT];
     float m_run = -SB_INF, l_run = 0.f;
@@ -871,20 +898,62 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void paged_attn_shared_ker
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
     const int krow = (li & 19) | ((li & 4) << 1) | ((li & 8) >> 1);   // row li of a key tile is key krow of it
     const int kswz = PPK == 16 ? (krow & 15) : ((krow >> 1) & 7);
+    const auto seen = [&](int j, int t) {   // tiles t .. of turn j, by a query of the wave
+        if (GROUPS * j + grp >= steps.n) return false;
+        const int k = steps.at(GROUPS * j + grp) * CH + 32 * t;
+        return some_see(w, k, k + 32 * KT);
+    };
+
+    f32x16 st[KT];
+    bf16x8 op[PD];
+    auto scores = [&](int j, int t) {   // of the keys of turn j's tiles t ..
+        const uint16_t* const k = kv_s[grp][0][j & 1] + t * 32 * HD;
+        auto read = [&](int n) {   // k step n / KT of tile n % KT
+            op[n % PD] = *reinterpret_cast<const bf16x8*>(&k[((n % KT) * 32 + krow) * HD + (((n / KT) * 2 + lh) ^ kswz) * 8]);
+        };
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) st[kt][r] = 0.f;
+#pragma unroll
+        for (int n = 0; n < PD; ++n) read(n);
+#pragma unroll
+        for (int n = 0; n < NK; n += KT) {
+#pragma unroll
+            for (int x = 0; x < PARTS; ++x) {
+                const bf16x8 qx = x < PARTS - IN_LDS ? qo[x < PARTS - IN_LDS ? x : 0][n / KT] : q_s[IN_LDS ? ((x - 1) * KS + n / KT) * 256 + wave * 64 + lane : 0];
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) st[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[(n + kt) % PD], qx, st[kt], 0, 0, 0);
+            }
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+                if (n + kt + PD < NK) read(n + kt + PD);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
 
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    for (int i = 0; i < steps.n; ++i) {
-        const int key0 = steps.at(i) * CH, buf = i & 1;
-        if (i + 1 < steps.n) {
-            issue(buf ^ 1);
-            lookup(i + 2);
-        }
-        auto v_at = [&](int page, int dt) {   // dims 32 dt + li, keys 8 lh .. of a page of the step
-            const int slot = (dt * 32 + li) * 2 + lh;
-            return *reinterpret_cast<const bf16x8*>(&v_s[buf][page * SLAB + (slot ^ ((slot >> 4) & 1)) * 8]);
+    if constexpr (GROUPS == 2) {
+        if (grp == 1 && turns > 0 && seen(0, 0)) scores(0, 0);
+        __syncthreads();   // (every wave is done with the first keys of group 1)
+    }
+#pragma unroll 1
+    for (int j = 0; j < turns; ++j) {
+        const int buf = j & 1;
+        // K: group 0 the next turn's, group 1 the one's after that, whose place this turn's scores have left
+        issue(kbase, koff, kv_s[grp][0][grp ? buf : buf ^ 1], pages_k);
+        issue(vbase, voff, kv_s[grp][1][buf ^ 1], pages_v);
+        pages_v = grp ? pages_k : lookup(j + 2);
+        pages_k = grp ? lookup(j + 3) : pages_v;
+        const int ka = steps.at(GROUPS * j) * CH, kb = steps.at(GROUPS == 2 && 2 * j + 1 < steps.n ? 2 * j + 1 : GROUPS * j) * CH;   // the groups' keys
+        const int key0 = grp ? kb : ka;
+        uint16_t* const v_s = kv_s[grp][1][buf];
+        auto v_at = [&](int n) {   // page n / DT, dims 32 (n % DT) + li, keys 8 lh ..
+            const int slot = ((n % DT) * 32 + li) * 2 + lh;
+            return *reinterpret_cast<const bf16x8*>(&v_s[(n / DT) * SLAB + (slot ^ ((slot >> 4) & 1)) * 8]);
         };
-        if (!all_see(all, key0, key0 + CH)) {
+        if (!all_see(all, ka, ka + CH) || !all_see(all, kb, kb + CH)) {
             // Some query does not see some key: its value must not be an infinity or NaN in the product.  Slots past the last key are
             // made zeros; if a value that some query sees is one (a thread looks at the pieces that it staged), its product
             // with who sees it is taken here and a zero left in its place.
@@ -893,25 +962,25 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void paged_attn_shared_ker
             for (int k = 0; k < NL; ++k) {
                 const int slot = k * NT + tid;
                 const int vk = key0 + (slot / (SB_KV_BLOCK * PPK)) * SB_KV_BLOCK + ((slot ^ (slot >> 4)) & 1) * 8;   // keys vk .. vk + 7 of one dim
-                uint4 v = *reinterpret_cast<uint4*>(&v_s[buf][slot * 8]);
+                uint4 v = *reinterpret_cast<uint4*>(&v_s[slot * 8]);
                 if (vk + 8 > s.len) {
                     uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) u[e] = vk + 2 * e + 1 < s.len ? u[e] : vk + 2 * e < s.len ? u[e] & 0xffffu : 0u;
                     v = make_uint4(u[0], u[1], u[2], u[3]);
-                    *reinterpret_cast<uint4*>(&v_s[buf][slot * 8]) = v;
+                    *reinterpret_cast<uint4*>(&v_s[slot * 8]) = v;
                 }
                 most(v, top);
             }
-            if (not_finite(top) && lane == 0) sick_s = i + 1;
+            if (not_finite(top) && lane == 0) sick_s = j + 1;
             __syncthreads();
-            if (sick_s == i + 1) {
+            if (sick_s == j + 1) {
 #pragma unroll 1
                 for (int x = 0; x < NPG; ++x) {
                     const bf16x8 see = sight(q, key0 + 16 * x + 8 * lh);
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) {
-                        uint4 v = __builtin_bit_cast(uint4, v_at(x, dt)), bad;
+                        uint4 v = __builtin_bit_cast(uint4, v_at(x * DT + dt)), bad;
                         set_apart(v, bad);
                         o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, bad), see, o[dt], 0, 0, 0);
                     }
@@ -919,7 +988,7 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void paged_attn_shared_ker
                 __syncthreads();
 #pragma unroll 1
                 for (int k = 0; k < NL; ++k) {
-                    uint4* const at = reinterpret_cast<uint4*>(&v_s[buf][(k * NT + tid) * 8]);
+                    uint4* const at = reinterpret_cast<uint4*>(&v_s[(k * NT + tid) * 8]);
                     uint4 v = *at, bad;
                     set_apart(v, bad);
                     *at = v;
@@ -928,68 +997,86 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void paged_attn_shared_ker
             }
         }
 #pragma unroll 1
-        for (int t0 = 0; t0 < 2; t0 += KT) {   // tiles t0 .. t0 + KT - 1 of the step
-            const int tk = key0 + 32 * t0;
-            if (!some_see(w, tk, tk + 32 * KT)) continue;
-            f32x16 st[KT];
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) st[kt][r] = 0.f;
-            bf16x8 op[PD];
-            auto read_k = [&](int n) {   // k step n / KT of tile n % KT
-                op[n % PD] = *reinterpret_cast<const bf16x8*>(&k_s[buf][(((t0 + n % KT) * 32 + krow) * PPK + (((n / KT) * 2 + lh) ^ kswz)) * 8]);
-            };
-#pragma unroll
-            for (int n = 0; n < PD; ++n) read_k(n);
-#pragma unroll
-            for (int n = 0; n < KT * KS; n += KT) {
-#pragma unroll
-                for (int x = 0; x < PARTS; ++x)
-#pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) st[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[(n + kt) % PD], qo[x][n / KT], st[kt], 0, 0, 0);
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
-                    if (n + kt + PD < KT * KS) read_k(n + kt + PD);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+        for (int t = 0; t < CH / 32; t += KT) {
+            if (!seen(j, t)) continue;
+            const int tk = key0 + 32 * t;
+            if (grp == 0) scores(j, t);
             shape_scores<PARTS, KT, SHAPED>(a, q, tk, lh, st);
             if (!all_see(w, tk, tk + 32 * KT)) mask_scores<KT>(q, w, tk, lh, st);
-            auto read_v = [&](int n) { op[n % PD] = v_at(2 * t0 + n / DT, n % DT); };
+            auto read = [&](int n) { op[n % PD] = v_at(2 * t * DT + n); };
 #pragma unroll
-            for (int n = 0; n < PD; ++n) read_v(n);
+            for (int n = 0; n < PD; ++n) read(n);
             bf16x8 p[PARTS][2 * KT];
             soft_max<PARTS, KT, DT>(st, mul, o, m_run, l_run, p);
 #pragma unroll
-            for (int n = 0; n < 2 * KT * DT; n += 2) {
+            for (int n = 0; n < NV; n += 2) {
 #pragma unroll
                 for (int y = 0; y < PARTS; ++y)
 #pragma unroll
                     for (int x = 0; x < 2; ++x) o[(n + x) % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[(n + x) % PD], p[y][n / DT], o[(n + x) % DT], 0, 0, 0);
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
-                    if (n + x + PD < 2 * KT * DT) read_v(n + x + PD);
+                    if (n + x + PD < NV) read(n + x + PD);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        __builtin_amdgcn_s_waitcnt(0);   // this wave's pieces of the next step have landed
-        __syncthreads();                 // ... and everybody's; every wave is done with this step
+        if (GROUPS == 2 && grp == 1 && seen(j + 1, 0)) scores(j + 1, 0);
+        __builtin_amdgcn_s_waitcnt(0);   // this wave's pieces have landed
+        __syncthreads();                 // ... and everybody's; every wave is done with this turn
     }
-    const float l = lanes_sum<32, 32>(l_run), inv_l = l == 0.f ? 0.f : 1.0f / l;
+    const float l_own = lanes_sum<32, 32>(l_run);
+    if constexpr (GROUPS == 1) {
+        const float inv_l = l_own == 0.f ? 0.f : 1.0f / l_own;
+        if (!q.valid) return;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                store_out4<HD>(a, q, dt * 32 + 2 * r + 4 * lh, make_float4(o[dt][r] * inv_l, o[dt][r + 1] * inv_l, o[dt][r + 2] * inv_l, o[dt][r + 3] * inv_l));
+        return;
+    }
+    // ---- the groups' results at one reference point: each keeps half of the dims and gives the other half away
+    if (lh == 0) { ml_s[grp][wave][li][0] = m_run; ml_s[grp][wave][li][1] = l_own; }
+    f32x4* const x_s = reinterpret_cast<f32x4*>(&kv_s[0][0][0][0]);   // [group][wave][dims][64 lanes]
+    constexpr int HALF = DT / 2 * 4;
+#pragma unroll
+    for (int dt = 0; dt < DT / 2; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = grp ? o[dt][r + e] : o[dt + DT / 2][r + e];
+            x_s[((grp * 4 + wave) * HALF + dt * 4 + r / 4) * 64 + lane] = v;
+        }
+    __syncthreads();
+    const float mx = fmaxf(m_run, ml_s[GROUPS - 1 - grp][wave][li][0]), ref = mx == -SB_INF ? 0.f : mx;
+    const float f = __builtin_amdgcn_exp2f(m_run - ref), h = __builtin_amdgcn_exp2f(ml_s[GROUPS - 1 - grp][wave][li][0] - ref);
+    const float l = l_own * f + ml_s[GROUPS - 1 - grp][wave][li][1] * h, inv_l = l == 0.f ? 0.f : 1.0f / l;
     if (!q.valid) return;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+    for (int dt = 0; dt < DT / 2; ++dt)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4)
-            store_out4<HD>(a, q, dt * 32 + 2 * r + 4 * lh, make_float4(o[dt][r] * inv_l, o[dt][r + 1] * inv_l, o[dt][r + 2] * inv_l, o[dt][r + 3] * inv_l));
+        for (int r = 0; r < 16; r += 4) {
+            const f32x4 u = x_s[(((GROUPS - 1 - grp) * 4 + wave) * HALF + dt * 4 + r / 4) * 64 + lane];
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = ((grp ? o[dt + DT / 2][r + e] : o[dt][r + e]) * f + u[e] * h) * inv_l;
+            store_out4<HD>(a, q, (dt + grp * (DT / 2)) * 32 + 2 * r + 4 * lh, make_float4(v[0], v[1], v[2], v[3]));
+        }
 }
 
-// How the keys of a call are split: 32-key steps per block (a multiple of the four waves) and the most chunks that gives.
+// Which form a call takes, and how its keys are split.  Blocks of 128 queries read a quarter of what blocks of 32 do, but a few of them leave the card
+// idle and a long one to wait for.  From 192 of them on for bf16 rows, 512 for float rows (whose products take three times as long for the
+// same reads), shared / apart: 32 heads of 128 over 8, bf16: 128 blocks (512 rows) 21.1 / 17.9 us, 256 (1024 rows) 33.7 / 41.7, 512 (2048) 67.7 /
+// 117.9; float: 256 56.1 / 51.3, 512 120.8 / 150.3; heads of 64, float: 256 40.0 / 32.0, 512 81.6 / 82.7, as 4 x 512 rows 33.8 / 37.0.
+// Sequences of a few rows, which would leave most of such a block empty, are taken apart.
+//   Taken apart, a block has as many 32-key steps (a multiple of its four waves) as give some 512 blocks, 64 at most: six rows behind
+// 131000 keys, 64 steps 106 us, 16 steps 172 when a CU had one block; 64 sequences of up to 8000 keys, 32 / 64 / 128 steps 251 / 243 / 272 us.
 struct AttnPlan { bool shared; int64_t tiles; int steps, chunks; };
-static AttnPlan attn_plan(const PagedKv& kv, int32_t n_heads) {
+static AttnPlan attn_plan(const PagedKv& kv, int32_t n_heads, bool fp32) {
     const int64_t G = n_heads / kv.n_kv_heads, total = (kv.max_len + 31) / 32;
     AttnPlan p;
-    p.shared = (int64_t)kv.n_rows * n_heads / 128 >= 320 && kv.n_rows * G >= 64 * kv.n_seq;
+    p.shared = (int64_t)kv.n_rows * n_heads / 128 >= (fp32 ? 512 : 192) && kv.n_rows * G >= 64 * (int64_t)kv.n_seq;
     if (p.shared) {
         p.tiles = kv.n_rows * G / 128 + kv.n_seq;
         p.steps = 0;
@@ -999,25 +1086,26 @@ static AttnPlan attn_plan(const PagedKv& kv, int32_t n_heads) {
     p.tiles = kv.n_rows * G / 32 + kv.n_seq;
     const int64_t want = (p.tiles * kv.n_kv_heads * total + 511) / 512;
     p.steps = (int)(want < 4 ? 4 : want > 64 ? 64 : (want + 3) / 4 * 4);
-    if (total / p.steps > 512) p.steps = (int)((total / 512 + 3) / 4 * 4);
+    const int64_t most = 4096 / (p.tiles * kv.n_kv_heads) + 1;   // chunks: what they leave stays below some 70 MB
+    if (total > most * p.steps) p.steps = (int)((total + most - 1) / most + 3) / 4 * 4;
     p.chunks = (int)((total + p.steps - 1) / p.steps);
     return p;
 }
 
-size_t paged_attention_scratch(const PagedKv& kv, int32_t n_heads) {
-    const AttnPlan p = attn_plan(kv, n_heads);
+size_t paged_attention_scratch(const PagedKv& kv, int32_t n_heads) {   // (of either type: float rows are taken apart longer)
+    const AttnPlan p = attn_plan(kv, n_heads, true);
     return p.chunks > 1 ? Partials::bytes((int64_t)kv.n_rows * n_heads, p.chunks, kv.head_dim) : 0;
 }
 
 hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t st) {
-    const AttnPlan p = attn_plan(a.kv, a.n_heads);
+    const AttnPlan p = attn_plan(a.kv, a.n_heads, a.x_dtype == SB_FP32);
     const auto go = [&](auto hd_c) {
         constexpr int HD = decltype(hd_c)::value;
         const dim3 grid((unsigned)(p.tiles * a.kv.n_kv_heads), p.chunks);
         const bool shaped = a.cap > 0.f || a.slopes;
         if (p.shared)
             return launch(a.x_dtype == SB_FP32 ? (shaped ? &paged_attn_shared_kernel<HD, 3, true> : &paged_attn_shared_kernel<HD, 3, false>)
-                                               : (shaped ? &paged_attn_shared_kernel<HD, 1, true> : &paged_attn_shared_kernel<HD, 1, false>), grid, 256, st, a);
+                                               : (shaped ? &paged_attn_shared_kernel<HD, 1, true> : &paged_attn_shared_kernel<HD, 1, false>), grid, a.x_dtype == SB_FP32 ? 256 * SharedForm<HD, 3>::GROUPS : 256, st, a);
         const hipError_t e = launch(a.x_dtype == SB_FP32 ? &paged_attn_apart_kernel<HD, 3> : &paged_attn_apart_kernel<HD, 1>, grid, 256, st, a, p.steps);
         if (e != hipSuccess || p.chunks == 1) return e;
         return launch(&paged_attn_merge_kernel<HD>, dim3(a.kv.n_rows * a.n_heads), 256, st, a, p.chunks);

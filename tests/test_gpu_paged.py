@@ -299,8 +299,8 @@ ATT_SHAPES = [
     ([300], [1111], 16, 4, 128),
     ([700, 257], [700, 400], 40, 40, 64),
     # enough rows that blocks of 128 queries fill the card
-    ([1500, 1200, 70], [1500, 1333, 900], 16, 4, 64),
-    ([1000, 40, 300], [1601, 41, 777], 32, 16, 128),
+    ([1500, 1200, 70], [1500, 1333, 900], 24, 4, 64),
+    ([1000, 40, 300], [1601, 41, 777], 64, 16, 128),
 ]
 
 
