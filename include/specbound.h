@@ -474,7 +474,9 @@ enum { SB_ROPE_HALF = 0, SB_ROPE_INTERLEAVED = 1 };
  * (2 i, 2 i + 1) with SB_ROPE_INTERLEAVED, (a, b) -> (a c - b s, b c + a s) with c, s from rope_cos /
  * rope_sin (device [n_pos][rot_dim / 2]; any table, see sb_rope_table_scaled_host).  Rotated q goes to
  * q_out [n_rows][ld_q] in x_dtype, rotated k and v, rounded to bf16, to the pages of `layer`.  All in
- * float, each output rounded once.  Two rows of a call must not be at one place of the pool.
+ * float, each output rounded once.  Two rows of a call must not be at one place of the pool, and nobody else
+ * may write to a page meanwhile that it appends to (v goes out eight keys of a dim together, those that
+ * are not new as they were).
  * A row at a position outside 0 .. n_pos - 1 is neither read nor written (n_pos is not looked at with
  * rot_dim 0); a position of max_len or more cannot arise.  q_out may be qkv itself (same ld), else it
  * must not overlap it.  Operands 16-byte aligned, rows a multiple of 16 bytes apart. */

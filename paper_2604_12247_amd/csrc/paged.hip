@@ -55,8 +55,15 @@ __device__ __forceinline__ void load4(const float* p, float (&x)[4]) {
     const float4 v = *reinterpret_cast<const float4*>(p);
     x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
 }
-__device__ __forceinline__ void load4(const uint16_t* p, float (&x)[4]) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
+// The same of rows that are read once: past the caches' usual replacement (8100 rows of 48 heads 51 -> 47 us).
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void load_row4(const float* p, float (&x)[4]) {
+    const f32x4v v = __builtin_nontemporal_load(reinterpret_cast<const f32x4v*>(p));
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+}
+__device__ __forceinline__ void load_row4(const uint16_t* p, float (&x)[4]) {
+    const u32x2v v = __builtin_nontemporal_load(reinterpret_cast<const u32x2v*>(p));
     x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xffff0000u);
     x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xffff0000u);
 }
@@ -73,9 +80,10 @@ __device__ __forceinline__ uint32_t load_pair(const uint16_t* p) { return *reint
 // heads, or ROPE_V v heads.  Sequence b's pages are tiles row_start[b] / 16 + 2 b .., as many as its rows can touch.
 //   q and k: HD / 8 lanes a head, eight values a lane -- the two ends of four pairs, so that norm and rotation stay within
 // the lane but for the sum of squares; ROPE_U heads a thread in flight.
-//   v: a thread takes two dims and eight slots, and its page half leaves as 16-byte pieces of the transposed slab where all
-// eight are new.
-constexpr int ROPE_U = 4;
+//   v: a thread takes two dims and eight slots, which leave as 16-byte pieces of the transposed slab; where not all eight are new, the
+// others are read and written back (stored by two bytes, 220 rows in 48 sequences of 32 v heads took 13.0 us, so 10.4; 5.8
+// without v: two pages a sequence are touched all over for them).
+constexpr int ROPE_U = 2;
 
 template <int HD, typename XT>
 __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a, int qk_heads, int qk_slices) {
@@ -112,8 +120,8 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a, int 
                 r[k] = i / nh;
                 head[k] = h0 + i - r[k] * nh;
                 const XT* p = x + (row0 + r[k]) * a.ld_qkv + head[k] * HD;
-                load4(p + dA, u[k][0]);
-                load4(p + dB, u[k][1]);
+                load_row4(p + dA, u[k][0]);
+                load_row4(p + dB, u[k][1]);
             }
 #pragma unroll
             for (int k = 0; k < ROPE_U; ++k) {
@@ -190,12 +198,17 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a, int 
         *reinterpret_cast<uint4*>(dst) = make_uint4(lo2[0], lo2[1], lo2[2], lo2[3]);
         *reinterpret_cast<uint4*>(dst + SB_KV_BLOCK) = make_uint4(hi2[0], hi2[1], hi2[2], hi2[3]);
     } else {
+        const uint4 a0 = *reinterpret_cast<const uint4*>(dst), a1 = *reinterpret_cast<const uint4*>(dst + SB_KV_BLOCK);
+        uint32_t x0[4] = {a0.x, a0.y, a0.z, a0.w}, x1[4] = {a1.x, a1.y, a1.z, a1.w};
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             if (t0 + e >= s_lo && t0 + e < s_hi) {
-                dst[e] = (uint16_t)w[e];
-                dst[SB_KV_BLOCK + e] = (uint16_t)(w[e] >> 16);
+                const int sh = (e & 1) * 16;
+                x0[e >> 1] = (x0[e >> 1] & ~(0xffffu << sh)) | ((w[e] & 0xffffu) << sh);
+                x1[e >> 1] = (x1[e >> 1] & ~(0xffffu << sh)) | ((w[e] >> 16) << sh);
             }
+        *reinterpret_cast<uint4*>(dst) = make_uint4(x0[0], x0[1], x0[2], x0[3]);
+        *reinterpret_cast<uint4*>(dst + SB_KV_BLOCK) = make_uint4(x1[0], x1[1], x1[2], x1[3]);
     }
 }
 
@@ -1114,28 +1127,19 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------- page copies
-// A block copies COPY_PIECE bytes of a page, four 16-byte loads a thread in flight.  grid (pages x pieces of a page, slabs).
-constexpr int COPY_PIECE = 16384;
+// 16 bytes a thread, nothing more: with four loads a thread in flight (16 KB pieces) a fork of 10 MB took 16.7 us and a compaction of 870 MB
+// (read and written) 160, with one 4.2 and 145 (6.0 TB/s; a plain copy of 1 GB to the next runs at 4.7).  grid (pages x pieces of a page, slabs).
+constexpr int COPY_PIECE = 4096;
 __global__ __launch_bounds__(256) void copy_pages_kernel(CopyPagesArgs a, int pieces) {
     const int page = blockIdx.x / pieces, piece = blockIdx.x - page * pieces;
     const uint4* s = reinterpret_cast<const uint4*>(a.src + blockIdx.y * a.src_slab + a.from[page] * a.page_bytes);
     uint4* d = reinterpret_cast<uint4*>(a.dst + blockIdx.y * a.dst_slab + a.to[page] * a.page_bytes);
-    const size_t n = a.page_bytes / 16, i = (size_t)piece * (COPY_PIECE / 16) + threadIdx.x;
-    constexpr int U = COPY_PIECE / (16 * 256);
-    if (i + (U - 1) * 256 < n) {
-        uint4 v[U];
-#pragma unroll
-        for (int k = 0; k < U; ++k) v[k] = s[i + k * 256];
-#pragma unroll
-        for (int k = 0; k < U; ++k) d[i + k * 256] = v[k];
-    } else {
-        for (int k = 0; k < U; ++k)
-            if (i + k * 256 < n) d[i + k * 256] = s[i + k * 256];
-    }
+    const size_t i = (size_t)piece * (COPY_PIECE / 16) + threadIdx.x;
+    if (i < a.page_bytes / 16) d[i] = s[i];
 }
 hipError_t launch_copy_pages(const CopyPagesArgs& a, int32_t n, int32_t n_slabs, hipStream_t st) {
     const size_t pieces = (a.page_bytes + COPY_PIECE - 1) / COPY_PIECE;
-    if (pieces * n > 0x7fffffff) return hipErrorInvalidValue;
+    if (pieces > 0x7fffffff / (size_t)n) return hipErrorInvalidValue;
     return launch(&copy_pages_kernel, dim3((unsigned)(pieces * n), n_slabs), 256, st, a, (int)pieces);
 }
 
