@@ -289,6 +289,7 @@ struct PagedAttnArgs {
     void* out;
     int64_t ld_q, ld_out;
     int32_t x_dtype, n_heads, group;
+    int32_t group_shift;   // group = 1 << group_shift, or -1: set by launch_paged_attention
     float scale, cap;
     const float* slopes;
     int32_t window;

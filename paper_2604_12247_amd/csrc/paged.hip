@@ -266,6 +266,9 @@ __device__ __forceinline__ SeqRows tile_seq(const PagedAttnArgs& a, int t, int& 
     return s;
 }
 
+// Row of query qq of a sequence (heads of one kv head's group per row).
+__device__ __forceinline__ int row_of(const PagedAttnArgs& a, int qq) { return a.group_shift >= 0 ? qq >> a.group_shift : qq / a.group; }
+
 // A lane's query: where it is, and the keys that it sees as two ranges [a0, a0 + an), [b0, b0 + bn).
 struct Query {
     int row, head, pos, a0, b0;
@@ -276,10 +279,11 @@ struct Query {
 // What all 32 queries of a wave see (whole ranges), and bounds of what any of them does; scalars.
 struct Reach { int a_lo, a_hi, b_lo, b_hi, a0_max, a1_min, b0_max, b1_min; };
 
-__device__ __forceinline__ Query lane_query(const PagedAttnArgs& a, const SeqRows& s, int g, int qq, Reach& w) {
+// Of query qw + lane % 32 of the sequence; qw is the wave's first, uniform.
+__device__ __forceinline__ Query lane_query(const PagedAttnArgs& a, const SeqRows& s, int g, int qw, int li, Reach& w) {
     Query q;
-    const int G = a.group, r = qq / G;
-    q.valid = qq < s.n * G;
+    const int G = a.group, qq = qw + li, nq = s.n * G, r = row_of(a, qq);
+    q.valid = qq < nq;
     q.row = s.r0 + (q.valid ? r : 0);
     q.head = g * G + (q.valid ? qq - r * G : 0);
     q.pos = s.len - s.n + q.row - s.r0;
@@ -289,10 +293,21 @@ __device__ __forceinline__ Query lane_query(const PagedAttnArgs& a, const SeqRow
     q.bn = q.valid && v.b1 > v.b0 ? v.b1 - v.b0 : 0;
     q.slope2 = a.slopes ? a.slopes[q.head] * LOG2E : 0.f;
     const int big = 0x7fffffff;
-    w.a_lo = half_min(q.an ? v.a0 : big); w.a_hi = half_max(q.an ? v.a1 : 0);
-    w.b_lo = half_min(q.bn ? v.b0 : big); w.b_hi = half_max(q.bn ? v.b1 : 0);
-    w.a0_max = half_max(q.valid ? v.a0 : 0); w.a1_min = half_min(q.valid ? v.a1 : big);
-    w.b0_max = half_max(q.valid ? v.b0 : 0); w.b1_min = half_min(q.valid ? v.b1 : big);
+    if (a.doc_start) {
+        w.a_lo = half_min(q.an ? v.a0 : big); w.a_hi = half_max(q.an ? v.a1 : 0);
+        w.b_lo = half_min(q.bn ? v.b0 : big); w.b_hi = half_max(q.bn ? v.b1 : 0);
+        w.a0_max = half_max(q.valid ? v.a0 : 0); w.a1_min = half_min(q.valid ? v.a1 : big);
+        w.b0_max = half_max(q.valid ? v.b0 : 0); w.b1_min = half_min(q.valid ? v.b1 : big);
+    } else {   // without documents the first and the last row tell (eight reductions over the lanes less)
+        const bool any = qw < nq;
+        const int last = s.len - s.n + row_of(a, qw + 31 < nq ? qw + 31 : nq - 1), first = s.len - s.n + row_of(a, qw);
+        const int pre = a.prefix_len ? clampi(a.prefix_len[s.b], 0, s.len) : 0, win = a.window > 0 ? a.window : big;
+        const auto from = [&](int p) { return p >= win ? p + 1 - win : 0; };
+        w.a_lo = any && pre ? 0 : big; w.a_hi = any ? pre : 0;
+        w.b_lo = any && last >= 0 ? from(first) : big; w.b_hi = any && last >= 0 ? last + 1 : 0;
+        w.a0_max = 0; w.a1_min = any ? pre : big;
+        w.b0_max = any ? from(last) : 0; w.b1_min = any ? (first >= 0 ? first + 1 : 0) : big;
+    }
     return q;
 }
 __device__ __forceinline__ bool all_see(const Reach& w, int k0, int k1) {   // keys k0 .. k1 - 1, every query
@@ -327,36 +342,30 @@ __device__ __forceinline__ Steps steps_of(const Reach& w) {
     return t;
 }
 
-// Eight values as PARTS bf16 B operands: one for bf16 rows, three for float rows (8 + 8 + 8 bits: all of them).
+// Eight floats as PARTS bf16 operands: with three, all of their 24 bits (8 + 8 + 8).
 template <int PARTS>
-__device__ __forceinline__ void split8(const void* rows, int64_t at, bf16x8 (&op)[PARTS]) {
+__device__ __forceinline__ void split8(float4 x, float4 y, bf16x8 (&op)[PARTS]) {
+    float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            w[e] = pack_bf16(f[2 * e], f[2 * e + 1]);
+            f[2 * e] -= __uint_as_float(w[e] << 16);
+            f[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+        }
+        op[i] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+    }
+}
+// Eight values of a row as operands: bf16 rows as they are, float rows in three parts.
+template <int PARTS>
+__device__ __forceinline__ void load8_split(const void* rows, int64_t at, bf16x8 (&op)[PARTS]) {
     if constexpr (PARTS == 1) {
         op[0] = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const uint16_t*>(rows) + at);
     } else {
         const float* p = reinterpret_cast<const float*>(rows) + at;
-        const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
-        float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-#pragma unroll
-        for (int i = 0; i < PARTS; ++i) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                w[e] = pack_bf16(f[2 * e], f[2 * e + 1]);
-                f[2 * e] -= __uint_as_float(w[e] << 16);
-                f[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
-            }
-            op[i] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-        }
-    }
-}
-template <int HD, int PARTS>
-__device__ __forceinline__ void load_query(const PagedAttnArgs& a, const Query& q, int lh, bf16x8 (&op)[PARTS][HD / 16]) {
-#pragma unroll
-    for (int ks = 0; ks < HD / 16; ++ks) {
-        bf16x8 t[PARTS];
-        split8<PARTS>(a.q, (int64_t)q.row * a.ld_q + q.head * HD + lh * 8 + ks * 16, t);
-#pragma unroll
-        for (int i = 0; i < PARTS; ++i) op[i][ks] = t[i];
+        split8<PARTS>(*reinterpret_cast<const float4*>(p), *reinterpret_cast<const float4*>(p + 4), op);
     }
 }
 
@@ -564,7 +573,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_apart_kernel(PagedAttnArgs 
     const SeqRows s = tile_seq<32>(a, blockIdx.x / Hkv, q0);
     if (s.b < 0) return;
     Reach w;
-    const Query q = lane_query(a, s, g, q0 + li, w);
+    const Query q = lane_query(a, s, g, q0, li, w);
     const Steps steps = steps_of<32>(w);
     const bool split = gridDim.y > 1;
     const Partials part(a.scratch, (int64_t)a.kv.n_rows * a.n_heads, gridDim.y, HD);
@@ -604,6 +613,26 @@ __global__ __launch_bounds__(256, 2) void paged_attn_apart_kernel(PagedAttnArgs 
             for (int dt = 0; dt < DT; ++dt) vr[x][dt] = *reinterpret_cast<const uint4*>(p + dt * 32 * SB_KV_BLOCK);
         }
     };
+    // The queries: bf16 rows in registers; the three parts of float rows in LDS, made once for the four waves (in registers they would leave
+    // one block per CU), where the results go later.  They are requested before the first keys, so that they are not waited for behind them.
+    constexpr int NQ = PARTS == 1 ? KS : HD / 64;
+    bf16x8 qo[KS];
+    float4 qf[NQ][2];
+    bf16x8* const q_s = reinterpret_cast<bf16x8*>(&o_s[0][0][0][0]);   // [PARTS][KS][64 lanes]
+    static_assert(PARTS * KS * 64 * 16 <= (int)sizeof(o_s), "the queries fit where the results go");
+    if constexpr (PARTS == 1) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+            qo[ks] = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const uint16_t*>(a.q) + (int64_t)q.row * a.ld_q + q.head * HD + lh * 8 + ks * 16);
+    } else {
+        const int x = tid / 8, qq = q0 + x < s.n * a.group ? q0 + x : q0, r = row_of(a, qq);   // (past the end: the first one, not stored)
+        const float* p = reinterpret_cast<const float*>(a.q) + (int64_t)(s.r0 + r) * a.ld_q + (g * a.group + qq - r * a.group) * HD + tid % 8 * 8;
+#pragma unroll
+        for (int y = 0; y < NQ; ++y) {
+            qf[y][0] = *reinterpret_cast<const float4*>(p + 64 * y);
+            qf[y][1] = *reinterpret_cast<const float4*>(p + 64 * y + 4);
+        }
+    }
     int i = first + wave;
     const bool any = i < last;
     int cp0 = 0, cp1 = 0;   // pages of the step being worked on
@@ -614,27 +643,14 @@ __global__ __launch_bounds__(256, 2) void paged_attn_apart_kernel(PagedAttnArgs 
         cp0 = pg0; cp1 = pg1;
         if (i + W < last) lookup(i + W);
     }
-    // The queries: bf16 rows in registers; the three parts of float rows in LDS, made once for the four waves (in registers they would leave
-    // one block per CU), where the results go later.
-    bf16x8 qo[KS];
-    bf16x8* const q_s = reinterpret_cast<bf16x8*>(&o_s[0][0][0][0]);   // [PARTS][KS][64 lanes]
-    static_assert(PARTS * KS * 64 * 16 <= (int)sizeof(o_s), "the queries fit where the results go");
-    if constexpr (PARTS == 1) {
+    if constexpr (PARTS > 1) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            bf16x8 t[1];
-            split8<1>(a.q, (int64_t)q.row * a.ld_q + q.head * HD + lh * 8 + ks * 16, t);
-            qo[ks] = t[0];
-        }
-    } else {
-        const int x = tid / 8, qq = q0 + x < s.n * a.group ? q0 + x : q0, r = qq / a.group;   // (past the end: the first one, not stored)
-        const int64_t at = (int64_t)(s.r0 + r) * a.ld_q + (g * a.group + qq - r * a.group) * HD;
-#pragma unroll
-        for (int y = tid % 8; y < HD / 8; y += 8) {
+        for (int y = 0; y < NQ; ++y) {
             bf16x8 t[PARTS];
-            split8<PARTS>(a.q, at + y * 8, t);
+            split8<PARTS>(qf[y][0], qf[y][1], t);
+            const int at = tid % 8 + 8 * y;   // dims 8 at ..
 #pragma unroll
-            for (int z = 0; z < PARTS; ++z) q_s[(z * KS + y / 2) * 64 + (y & 1) * 32 + x] = t[z];
+            for (int z = 0; z < PARTS; ++z) q_s[(z * KS + at / 2) * 64 + (at & 1) * 32 + tid / 8] = t[z];
         }
         __syncthreads();
     }
@@ -736,20 +752,22 @@ __global__ __launch_bounds__(256, 2) void paged_attn_apart_kernel(PagedAttnArgs 
 #pragma unroll
     for (int v = 0; v < W; ++v) l += l_s[v][li] * __builtin_amdgcn_exp2f(m_s[v][li] - ref);
     const float f = __builtin_amdgcn_exp2f(m_run - ref);
+    if (any) {
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4)
-            *reinterpret_cast<f32x4*>(o_s[wave][dt * 4 + r / 4][lane]) = f32x4{o[dt][r] * f, o[dt][r + 1] * f, o[dt][r + 2] * f, o[dt][r + 3] * f};
+            for (int r = 0; r < 16; r += 4)
+                *reinterpret_cast<f32x4*>(o_s[wave][dt * 4 + r / 4][lane]) = f32x4{o[dt][r] * f, o[dt][r + 1] * f, o[dt][r + 2] * f, o[dt][r + 3] * f};
+    }
     __syncthreads();
     if (!q.valid) return;
+    const int nw = last - first < W ? last - first : W;   // waves that had a step
     const float inv_l = split ? 1.f : l == 0.f ? 0.f : 1.0f / l;
     const int64_t at = pair * gridDim.y + blockIdx.y;
     if (split && wave == 0 && lh == 0) { part.ml[2 * at] = mx; part.ml[2 * at + 1] = l; }
     for (int n = wave; n < NS; n += W) {   // (a lane finishes its own query: slot n holds dims 32 (n / 4) + 8 (n % 4) + 4 lh ..)
-        f32x4 v = *reinterpret_cast<const f32x4*>(o_s[0][n][lane]);
-#pragma unroll
-        for (int x = 1; x < W; ++x) {
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int x = 0; x < nw; ++x) {
             const f32x4 u = *reinterpret_cast<const f32x4*>(o_s[x][n][lane]);
             v[0] += u[0]; v[1] += u[1]; v[2] += u[2]; v[3] += u[3];
         }
@@ -768,13 +786,25 @@ __global__ __launch_bounds__(256) void paged_attn_merge_kernel(PagedAttnArgs a, 
     __shared__ float ls[NG];
     __shared__ __attribute__((aligned(16))) float os[NG][HD];
     const int tid = threadIdx.x, row = blockIdx.x / a.n_heads, head = blockIdx.x % a.n_heads, grp = tid / L, d = tid % L * 4;
-    const SeqRows s = find_rows(a.kv, [](int r0, int) { return r0; }, row);
-    if (s.b < 0 || row >= s.r0 + s.n) return;
     const Partials part(a.scratch, (int64_t)a.kv.n_rows * a.n_heads, chunks, HD);
     const int64_t pair = blockIdx.x, at = pair * chunks;
-    const int n = part.count[pair];
-    float mx = -SB_INF;
-    for (int c = tid; c < n; c += 256) mx = fmaxf(mx, part.ml[2 * (at + c)]);
+    // All that the first rounds may need is requested at once, before it is known how many chunks there are (what lies in the others is not used).
+    constexpr int U = 4;
+    const int n_all = part.count[pair];
+    const float m0 = part.ml[2 * (at + (tid < chunks ? tid : 0))];
+    float2 ml[U];
+    float4 pv[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int c = grp + NG * u < chunks ? grp + NG * u : 0;
+        ml[u] = *reinterpret_cast<const float2*>(part.ml + 2 * (at + c));
+        pv[u] = *reinterpret_cast<const float4*>(part.o + (at + c) * HD + d);
+    }
+    const SeqRows s = find_rows(a.kv, [](int r0, int) { return r0; }, row);
+    if (s.b < 0 || row >= s.r0 + s.n) return;
+    const int n = n_all;
+    float mx = tid < n ? m0 : -SB_INF;
+    for (int c = tid + 256; c < n; c += 256) mx = fmaxf(mx, part.ml[2 * (at + c)]);
     mx = wave_max(mx);
     if ((tid & 63) == 0) red[tid >> 6] = mx;
     __syncthreads();
@@ -782,14 +812,16 @@ __global__ __launch_bounds__(256) void paged_attn_merge_kernel(PagedAttnArgs a, 
     const float ref = mx == -SB_INF ? 0.f : mx;
     float l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int c = grp; c < n; c += NG) {
-        const float2 ml = *reinterpret_cast<const float2*>(part.ml + 2 * (at + c));
-        const float4 v = *reinterpret_cast<const float4*>(part.o + (at + c) * HD + d);
-        const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-        l += ml.y * f;
+    const auto take = [&](float2 x, float4 v) {
+        const float f = __builtin_amdgcn_exp2f(x.x - ref);
+        l += x.y * f;
         o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
-    }
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (grp + NG * u < n) take(ml[u], pv[u]);
+#pragma unroll 4
+    for (int c = grp + NG * U; c < n; c += NG) take(*reinterpret_cast<const float2*>(part.ml + 2 * (at + c)), *reinterpret_cast<const float4*>(part.o + (at + c) * HD + d));
     *reinterpret_cast<float4*>(&os[grp][d]) = o;
     if (d == 0) ls[grp] = l;
     __syncthreads();
@@ -838,7 +870,7 @@ __global__ __launch_bounds__((256 * SharedForm<HD, PARTS>::GROUPS), 2) void page
     const SeqRows s = tile_seq<BQ>(a, tiles - 1 - (int)(blockIdx.x / Hkv), q0);   // (a prompt's last rows see most: they start first)
     if (s.b < 0) return;
     Reach w;
-    const Query q = lane_query(a, s, g, q0 + wave * 32 + li, w);
+    const Query q = lane_query(a, s, g, q0 + wave * 32, li, w);
     if (lane == 0 && grp == 0) {
         int* const r = reach_s[wave];
         r[0] = w.a_lo; r[1] = w.b_lo; r[2] = w.a1_min; r[3] = w.b1_min;
@@ -896,7 +928,7 @@ __global__ __launch_bounds__((256 * SharedForm<HD, PARTS>::GROUPS), 2) void page
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         bf16x8 t[PARTS];
-        split8<PARTS>(a.q, (int64_t)q.row * a.ld_q + q.head * HD + lh * 8 + ks * 16, t);
+        load8_split<PARTS>(a.q, (int64_t)q.row * a.ld_q + q.head * HD + lh * 8 + ks * 16, t);
 #pragma unroll
         for (int x = 0; x < PARTS; ++x)
             if (x < PARTS - IN_LDS) qo[x][ks] = t[x];
@@ -1110,7 +1142,9 @@ size_t paged_attention_scratch(const PagedKv& kv, int32_t n_heads) {   // (of ei
     return p.chunks > 1 ? Partials::bytes((int64_t)kv.n_rows * n_heads, p.chunks, kv.head_dim) : 0;
 }
 
-hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t st) {
+hipError_t launch_paged_attention(const PagedAttnArgs& args, hipStream_t st) {
+    PagedAttnArgs a = args;
+    a.group_shift = (a.group & (a.group - 1)) == 0 ? __builtin_ctz(a.group) : -1;
     const AttnPlan p = attn_plan(a.kv, a.n_heads, a.x_dtype == SB_FP32);
     const auto go = [&](auto hd_c) {
         constexpr int HD = decltype(hd_c)::value;
