@@ -506,6 +506,13 @@ __device__ __forceinline__ void soft_max(f32x16 (&st)[KT], float mul, f32x16 (&o
     l_run += sum0 + sum1;
 }
 
+// Mask of the first n of eight bf16 values (n < 0: none, n > 8: all).
+__device__ __forceinline__ uint4 first_keys(int n) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = n > 2 * e + 1 ? 0xffffffffu : n > 2 * e ? 0xffffu : 0u;
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
 // Among eight bf16 values an infinity or NaN is one with all exponent bits set: the largest magnitudes so far, pairwise.
 __device__ __forceinline__ void most(uint4 v, u16x2v& top) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -698,14 +705,10 @@ __global__ __launch_bounds__(256, 2) void paged_attn_apart_kernel(PagedAttnArgs 
         if (key0 + 32 > s.len) {   // slots past the last key
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const int live = s.len - key0 - 16 * x - 8 * lh;   // keys of this lane's 8 that exist
+                const uint4 keep = first_keys(s.len - key0 - 16 * x - 8 * lh);   // of this lane's 8 keys, those that exist
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    uint32_t u[4] = {vr[x][dt].x, vr[x][dt].y, vr[x][dt].z, vr[x][dt].w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) u[e] = 2 * e + 1 < live ? u[e] : (2 * e < live ? u[e] & 0xffffu : 0u);
-                    vr[x][dt] = make_uint4(u[0], u[1], u[2], u[3]);
-                }
+                for (int dt = 0; dt < DT; ++dt)
+                    vr[x][dt] = make_uint4(vr[x][dt].x & keep.x, vr[x][dt].y & keep.y, vr[x][dt].z & keep.z, vr[x][dt].w & keep.w);
             }
         }
         bf16x8 p[PARTS][2];
@@ -765,14 +768,16 @@ __global__ __launch_bounds__(256, 2) void paged_attn_apart_kernel(PagedAttnArgs 
     const float inv_l = split ? 1.f : l == 0.f ? 0.f : 1.0f / l;
     const int64_t at = pair * gridDim.y + blockIdx.y;
     if (split && wave == 0 && lh == 0) { part.ml[2 * at] = mx; part.ml[2 * at + 1] = l; }
-    for (int n = wave; n < NS; n += W) {   // (a lane finishes its own query: slot n holds dims 32 (n / 4) + 8 (n % 4) + 4 lh ..)
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        for (int x = 0; x < nw; ++x) {
-            const f32x4 u = *reinterpret_cast<const f32x4*>(o_s[x][n][lane]);
-            v[0] += u[0]; v[1] += u[1]; v[2] += u[2]; v[3] += u[3];
-        }
-        const int col = (n >> 2) * 32 + (n & 3) * 8 + 4 * lh;
-        const float4 r = make_float4(v[0] * inv_l, v[1] * inv_l, v[2] * inv_l, v[3] * inv_l);
+    f32x4 sum[NS / W];   // (a lane finishes its own query: slot n holds dims 32 (n / 4) + 8 (n % 4) + 4 lh ..; a wave takes slots wave, wave + W ..)
+#pragma unroll
+    for (int k = 0; k < NS / W; ++k) sum[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int x = 0; x < nw; ++x)
+#pragma unroll
+        for (int k = 0; k < NS / W; ++k) sum[k] += *reinterpret_cast<const f32x4*>(o_s[x][wave + k * W][lane]);
+#pragma unroll
+    for (int k = 0; k < NS / W; ++k) {
+        const int n = wave + k * W, col = (n >> 2) * 32 + (n & 3) * 8 + 4 * lh;
+        const float4 r = make_float4(sum[k][0] * inv_l, sum[k][1] * inv_l, sum[k][2] * inv_l, sum[k][3] * inv_l);
         if (split) *reinterpret_cast<float4*>(part.o + at * HD + col) = r;
         else store_out4<HD>(a, q, col, r);
     }
@@ -1009,10 +1014,8 @@ __global__ __launch_bounds__((256 * SharedForm<HD, PARTS>::GROUPS), 2) void page
                 const int vk = key0 + (slot / (SB_KV_BLOCK * PPK)) * SB_KV_BLOCK + ((slot ^ (slot >> 4)) & 1) * 8;   // keys vk .. vk + 7 of one dim
                 uint4 v = *reinterpret_cast<uint4*>(&v_s[slot * 8]);
                 if (vk + 8 > s.len) {
-                    uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) u[e] = vk + 2 * e + 1 < s.len ? u[e] : vk + 2 * e < s.len ? u[e] & 0xffffu : 0u;
-                    v = make_uint4(u[0], u[1], u[2], u[3]);
+                    const uint4 keep = first_keys(s.len - vk);
+                    v = make_uint4(v.x & keep.x, v.y & keep.y, v.z & keep.z, v.w & keep.w);
                     *reinterpret_cast<uint4*>(&v_s[slot * 8]) = v;
                 }
                 most(v, top);

@@ -415,6 +415,80 @@ def test_large_and_equal_scores(shape):
             assert torch.equal(got[c.rows_of(b)].view(-1, hq, hd)[:, h].double(), want)
 
 
+@pytest.mark.parametrize("fp32", [True, False], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("rows,lens,hq,hkv,hd", [
+    ([i % 3 for i in range(300)], [i % 3 + i // 2 for i in range(300)], 4, 2, 64),
+    ([1] * 4200, [1 + i % 40 for i in range(4200)], 2, 1, 64),
+    ([40] * 80, [40 + 3 * i for i in range(80)], 16, 4, 64),
+    ([0] * 130 + [2], [9] * 130 + [700], 40, 1, 64),
+    ([3] * 65, [50] * 65, 6, 2, 128)], ids=lambda x: str(len(x)) if isinstance(x, list) else str(x))
+def test_many_sequences(rows, lens, hq, hkv, hd, fp32):
+    """More sequences than a wave looks at at once, some without rows; the same through the append."""
+    dt = torch.float32 if fp32 else torch.bfloat16
+    c = Case(rows, lens, hq, hkv, hd, dt, seed=len(rows), lead=1, tail=2, junk=math.nan)
+    cos, sin = (torch.from_numpy(t).to(DEV) for t in sb.rope_table_scaled(hd, 10000.0, max(lens)))
+    qkv = randn(5, c.n_rows, (hq + 2 * hkv) * hd).to(dt)
+    out = torch.full((c.n_rows, hq * hd), 7.0, dtype=dt, device=DEV)
+    q = sb.op_rope_append(c.kv, qkv, hq, cos, sin, out=out)
+    for b, ref, tol in rope_reference(c, qkv, cos, sin, False, None, None, 0.0):
+        x = q[c.rows_of(b)].double().view(-1, hq, hd)
+        assert ((x - ref[:, :hq]).abs() <= tol[:, :hq] + (0 if fp32 else UB) * (ref[:, :hq].abs() + tol[:, :hq])).all()
+    assert (q[0] == 7).all() and (q[-2:] == 7).all()
+    got = sb.op_paged_attention(c.kv, q, hq, out=torch.full_like(q, 7.0))
+    assert (got[0] == 7).all() and (got[-2:] == 7).all() and torch.isfinite(got.float()).all()
+    some = [b for b in range(len(rows)) if rows[b]][:: max(1, len(rows) // 24)]   # (the oracle on a few of them)
+    for b in some:
+        one = Case([rows[b]], [lens[b]], hq, hkv, hd, dt, seed=0)
+        k, v = c.cached(b)
+        pos = torch.arange(lens[b], device=DEV)
+        pg = one.table[0].long()[pos // PAGE]
+        one.pool[0, 0][pg, :, pos % PAGE] = k.to(torch.bfloat16)
+        one.pool[0, 1].view(one.n_pages, hkv, hd, PAGE)[pg, :, :, pos % PAGE] = v.to(torch.bfloat16)
+        want, tol = attention_reference(one, q[c.rows_of(b)])
+        assert ((got[c.rows_of(b)].double() - want).abs() <= tol).all(), b
+
+
+def test_table_rows_apart_and_lengths_above_max_len():
+    c = Case([3, 5], [100, 61], 8, 2, 128, torch.bfloat16, seed=2, table_ld=9)
+    wide = torch.full((2, 25), -1, dtype=torch.int32, device=DEV)
+    wide[:, :9] = c.table
+    kv = sb.Paged(c.pool, wide[:, :9], c.row_start, c.kv_len, n_rows=8)
+    assert kv.c.table_ld == 25
+    q = randn(3, 8, 1024).to(torch.bfloat16)
+    assert torch.equal(sb.op_paged_attention(kv, q, 8), sb.op_paged_attention(c.kv, q, 8))
+    # max_len cuts a longer sequence: its rows are the last max_len's
+    short = sb.Paged(c.pool, c.table, c.row_start, c.kv_len, n_rows=8, max_len=64)
+    c.kv_len[0] = 64
+    assert torch.equal(sb.op_paged_attention(short, q, 8), sb.op_paged_attention(c.kv, q, 8))
+
+
+@pytest.mark.parametrize("shape", [2, 5, 6])
+def test_scratch_needs_no_clearing(shape):
+    rows, lens, hq, hkv, hd = ATT_SHAPES[shape]
+    c = Case(rows, lens, hq, hkv, hd, torch.float32, seed=1)
+    q = randn(2, c.n_rows, hq * hd)
+    scratch = sb.paged_attention_scratch(c.kv, hq)
+    want = sb.op_paged_attention(c.kv, q, hq, scratch=scratch)
+    for fill in (0xff, 0x7f):
+        scratch.fill_(fill)
+        assert torch.equal(sb.op_paged_attention(c.kv, q, hq, scratch=scratch), want)
+
+
+@pytest.mark.parametrize("fp32", [True, False], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("shape", [3, 10, 12])
+def test_a_row_without_numbers_stays_alone(shape, fp32):
+    """NaN and infinite queries make their own outputs so, the others keep their bits."""
+    rows, lens, hq, hkv, hd = ATT_SHAPES[shape]
+    c = Case(rows, lens, hq, hkv, hd, torch.float32 if fp32 else torch.bfloat16, seed=3)
+    q = randn(4, c.n_rows, hq * hd).to(c.dtype)
+    want = sb.op_paged_attention(c.kv, q, hq)
+    bad = torch.arange(c.n_rows, device=DEV) % 5 == 2
+    q[bad] = math.nan
+    q[bad, 1] = math.inf
+    got = sb.op_paged_attention(c.kv, q, hq)
+    assert torch.equal(got[~bad], want[~bad]) and torch.isnan(got[bad]).all()
+
+
 def test_attention_pages_outside_the_pool_read_as_zeros():
     c = Case([2, 90], [70, 200], 8, 2, 64, torch.float32, seed=4, spare=0)
     zero = c.pool.clone()
