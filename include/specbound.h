@@ -453,7 +453,7 @@ int32_t sb_op_prompt_attention(const float *qkv, int32_t n_heads, int32_t n_kv_h
  *   What lies on the device is read when the kernels run (a captured call sees what stands there at
  * each replay), so it cannot be refused.  It is bounded instead: row_start is cut to 0 .. n_rows,
  * kv_len to 0 .. max_len; a page number outside 0 .. n_pages - 1 is never followed -- nothing is
- * written for it, its keys and values read as zeros.  row_start has to ascend.  Rows of no sequence
+ * written for it, its keys and values read as zeros.  row_start has to ascend (else it is open which rows are worked on).  Rows of no sequence
  * (before row_start[0], from row_start[n_seq] on) are neither read nor written. */
 typedef struct sb_paged {
     void *pool;               /* device, 16-byte aligned */
@@ -490,7 +490,7 @@ int32_t sb_op_rope_append(const sb_paged *kv, int32_t layer, const void *qkv, in
  * All zeros: plain causal attention. */
 typedef struct sb_attn_rule {
     float scale;               /* 0: 1 / sqrt(head_dim); else > 0 */
-    float softcap;             /* 0: none; else > 0 */
+    float softcap;             /* 0: none; else > 0 (1e30 at most, scale / softcap in 1e-34 .. 1e34) */
     const float *slopes;       /* NULL, or device [n_heads] */
     int32_t window;            /* 0: none; else the row's own key counts: window 1 sees that alone */
     const int32_t *prefix_len; /* NULL, or device [n_seq]: so many first keys are seen by every row (kv_len: all) */
@@ -504,7 +504,8 @@ typedef struct sb_attn_rule {
  * the product with V as bf16 (relative 2^-9 each, about what rounding the output costs).  SB_FP32: queries
  * and probabilities are carried with all 24 bits.  rule NULL: plain causal.  scratch: device, 256-byte aligned,
  * sb_op_paged_attention_scratch_bytes() bytes (SB_ENOMEM if fewer; needs no clearing; NULL where that is
- * 0).  The order of additions depends on the sizes in `kv`, not on the rows beside a row. */
+ * 0).  The same call gives the same bits: how the keys are split depends on the sizes in `kv`, and within a
+ * tile of rows on the keys that those rows see. */
 int32_t sb_op_paged_attention(const sb_paged *kv, int32_t layer, const void *q, int32_t x_dtype, int64_t ld_q, int32_t n_heads,
                               const sb_attn_rule *rule, void *out, int64_t ld_out, void *scratch, size_t scratch_bytes,
                               void *stream);
@@ -515,7 +516,7 @@ size_t sb_op_paged_attention_scratch_bytes(const sb_paged *kv, int32_t n_heads);
  * type).  The page lists are host memory, read during the call.  Page numbers out of range, a page written
  * twice, pools that overlap without being the same, and in one pool (src == dst, the same page count) a page
  * that is both written and read are refused; a page may be read any number of times.  Pools 16-byte aligned, page_bytes a
- * multiple of 16. */
+ * multiple of 16, 2^27 at most. */
 int32_t sb_op_copy_pages(void *dst, int32_t dst_n_pages, const void *src, int32_t src_n_pages, size_t page_bytes,
                          int32_t n_slabs, const int32_t *dst_pages, const int32_t *src_pages, int32_t n, void *stream);
 

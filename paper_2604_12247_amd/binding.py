@@ -813,6 +813,17 @@ def op_paged_attention(kv: Paged, q, n_heads: int, scale: float = 0.0, softcap: 
     return out
 
 
+def _page_list(pages):
+    """Page numbers as a dense int32 array; what int32 would change is refused."""
+    p = np.asarray(pages)
+    if p.dtype != np.int32:
+        if p.size and p.dtype.kind not in "iu":
+            raise TypeError(f"page numbers must be integers, not {p.dtype}")
+        if p.size and not (-2 ** 31 <= int(p.min()) and int(p.max()) < 2 ** 31):
+            raise ValueError("page numbers must fit 32 bits")
+    return np.ascontiguousarray(p, dtype=np.int32)
+
+
 def op_copy_pages(dst, src, dst_pages: Sequence[int], src_pages: Sequence[int]):
     """Page src_pages[i] of src -> page dst_pages[i] of dst, keys and values of all layers.  Pools [n_layers, 2, n_pages,
     n_kv_heads, SB_KV_BLOCK, head_dim] of any cache type, alike but for n_pages; dst may be src."""
@@ -822,7 +833,7 @@ def op_copy_pages(dst, src, dst_pages: Sequence[int], src_pages: Sequence[int]):
             raise ValueError(f"{name} must be a contiguous pool [n_layers, 2, n_pages, n_kv_heads, {SB_KV_BLOCK}, head_dim] on a GPU")
     if dst.shape[:2] != src.shape[:2] or dst.shape[3:] != src.shape[3:] or dst.dtype != src.dtype or dst.device != src.device:
         raise ValueError(f"pools differ: {tuple(dst.shape)} {dst.dtype} {dst.device}, {tuple(src.shape)} {src.dtype} {src.device}")
-    d, s = (np.ascontiguousarray(p, dtype=np.int32) for p in (dst_pages, src_pages))
+    d, s = _page_list(dst_pages), _page_list(src_pages)
     if d.ndim != 1 or d.shape != s.shape:
         raise ValueError("dst_pages and src_pages must be lists of one length")
     page_bytes, index = src.stride(2) * src.element_size(), src.get_device()
@@ -851,11 +862,11 @@ class Pages:
 
     def share(self, pages):
         """One more user for each page (a sequence forked without copying its full pages)."""
-        p = np.ascontiguousarray(pages, dtype=np.int32)
+        p = _page_list(pages)
         check(lib().sb_pages_share(self.h, p.ctypes.data, p.size))
 
     def release(self, pages):
-        p = np.ascontiguousarray(pages, dtype=np.int32)
+        p = _page_list(pages)
         check(lib().sb_pages_release(self.h, p.ctypes.data, p.size))
 
     def users(self, page: int) -> int:

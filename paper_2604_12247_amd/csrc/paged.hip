@@ -40,9 +40,6 @@ __device__ __forceinline__ SeqRows find_rows(const PagedKv& kv, First first, int
     return s;
 }
 
-__device__ __forceinline__ float load_x(const void* x, int64_t i, bool fp32) {
-    return fp32 ? reinterpret_cast<const float*>(x)[i] : bf2f(reinterpret_cast<const uint16_t*>(x)[i]);
-}
 __device__ __forceinline__ uint16_t round_bf16(float v) { return (uint16_t)pack_bf16(v, v); }   // (NaN stays one)
 __device__ __forceinline__ void store_x(void* x, int64_t i, bool fp32, float v) {
     if (fp32) reinterpret_cast<float*>(x)[i] = v;
@@ -261,7 +258,7 @@ __device__ __forceinline__ SeqRows tile_seq(const PagedAttnArgs& a, int t, int& 
     q0 = 0;
     if (s.b >= 0) {
         q0 = (t - (s.r0 * G / TQ + s.b)) * TQ;
-        if (q0 >= s.n * G) s.b = -1;
+        if ((unsigned)q0 >= (unsigned)(s.n * G)) s.b = -1;   // (below 0: only where row_start does not ascend)
     }
     return s;
 }
@@ -391,7 +388,7 @@ __device__ __forceinline__ void shape_scores(const PagedAttnArgs& a, const Query
     if constexpr (!SHAPED) return;
     if (a.cap > 0.f) {
         const float c2 = a.cap * LOG2E;
-        if constexpr (PARTS == 1) {   // tanh x = 1 - 2 / (exp 2x + 1): 2e-7 off at most, of scores that bf16 rows gave
+        if (PARTS == 1 && a.cap <= 512.f) {   // tanh x = 1 - 2 / (exp 2x + 1): 2e-7 off at most, so a score of bf16 rows 1e-4
             const float k = 2.f * LOG2E * a.scale / a.cap;
 #pragma unroll
             for (int t = 0; t < KT; ++t)
@@ -806,8 +803,8 @@ __global__ __launch_bounds__(256) void paged_attn_merge_kernel(PagedAttnArgs a, 
         pv[u] = *reinterpret_cast<const float4*>(part.o + (at + c) * HD + d);
     }
     const SeqRows s = find_rows(a.kv, [](int r0, int) { return r0; }, row);
-    if (s.b < 0 || row >= s.r0 + s.n) return;
-    const int n = n_all;
+    if (s.b < 0 || row < s.r0 || row >= s.r0 + s.n) return;
+    const int n = n_all < chunks ? n_all : chunks;   // (never more, unless what lies on the device changed since)
     float mx = tid < n ? m0 : -SB_INF;
     for (int c = tid + 256; c < n; c += 256) mx = fmaxf(mx, part.ml[2 * (at + c)]);
     mx = wave_max(mx);

@@ -111,8 +111,10 @@ int32_t sb_op_paged_attention(const sb_paged* kv, int32_t layer, const void* q, 
     int rc = paged_check(op, kv, layer, x_dtype, n_heads, &empty);
     if (rc) return rc;
     const sb_attn_rule r = rule ? *rule : sb_attn_rule{};
-    if (!(r.scale >= 0.f) || r.scale > 3e38f) return fail(SB_EINVAL, "%s: scale must be positive, or 0 for 1 / sqrt(head_dim)", op);
-    if (!(r.softcap >= 0.f) || r.softcap > 3e38f) return fail(SB_EINVAL, "%s: softcap must be positive, or 0 for none", op);
+    if (!(r.scale >= 0.f) || r.scale > 1e38f) return fail(SB_EINVAL, "%s: scale must be positive, or 0 for 1 / sqrt(head_dim)", op);
+    const float scale = r.scale > 0.f ? r.scale : 1.0f / sqrtf((float)kv->head_dim);
+    if (!(r.softcap >= 0.f) || r.softcap > 1e30f) return fail(SB_EINVAL, "%s: softcap must be positive and 1e30 at most, or 0 for none", op);
+    if (r.softcap > 0.f && !(scale / r.softcap >= 1e-34f && scale / r.softcap <= 1e34f)) return fail(SB_EINVAL, "%s: scale / softcap must be in 1e-34..1e34", op);
     if (r.window < 0) return fail(SB_EINVAL, "%s: window must be positive, or 0 for none", op);
     if (empty) return SB_OK;
     if (((uintptr_t)r.slopes | (uintptr_t)r.prefix_len | (uintptr_t)r.doc_start) & 3) return fail(SB_EINVAL, "%s: misaligned slopes, prefix_len or doc_start", op);
@@ -132,8 +134,7 @@ int32_t sb_op_paged_attention(const sb_paged* kv, int32_t layer, const void* q, 
     PagedAttnArgs a{};
     a.kv = device_kv(kv, layer);
     a.q = q; a.out = out; a.ld_q = ld_q; a.ld_out = ld_out; a.x_dtype = x_dtype; a.n_heads = n_heads; a.group = n_heads / kv->n_kv_heads;
-    a.scale = r.scale > 0.f ? r.scale : 1.0f / sqrtf((float)kv->head_dim);
-    a.cap = r.softcap; a.slopes = r.slopes; a.window = r.window; a.prefix_len = r.prefix_len; a.doc_start = r.doc_start;
+    a.scale = scale; a.cap = r.softcap; a.slopes = r.slopes; a.window = r.window; a.prefix_len = r.prefix_len; a.doc_start = r.doc_start;
     a.scratch = (float*)scratch;
     HIP_TRY(launch_paged_attention(a, (hipStream_t)stream));
     return SB_OK;
@@ -143,7 +144,7 @@ int32_t sb_op_copy_pages(void* dst, int32_t dst_n_pages, const void* src, int32_
                          const int32_t* dst_pages, const int32_t* src_pages, int32_t n, void* stream) {
     static const char* op = "op_copy_pages";
     if (dst_n_pages < 1 || src_n_pages < 1 || n_slabs < 1 || n_slabs > 65535 || n < 0) return fail(SB_EINVAL, "%s: bad count", op);
-    if (page_bytes < 16 || page_bytes % 16 || page_bytes > ((size_t)1 << 40)) return fail(SB_EINVAL, "%s: page_bytes must be a multiple of 16", op);
+    if (page_bytes < 16 || page_bytes % 16 || page_bytes > ((size_t)1 << 27)) return fail(SB_EINVAL, "%s: page_bytes must be a multiple of 16, 2^27 at most", op);
     if (n == 0) return SB_OK;
     if (!dst || !src || !dst_pages || !src_pages) return fail(SB_EINVAL, "%s: NULL argument", op);
     if (((uintptr_t)dst | (uintptr_t)src) & 15) return fail(SB_EINVAL, "%s: pools must be 16-byte aligned", op);

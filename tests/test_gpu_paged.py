@@ -343,6 +343,29 @@ def test_attention_rules(r, shape, fp32):
 
 
 @pytest.mark.parametrize("fp32", [True, False], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("cap", [1e6, 1e30])
+@pytest.mark.parametrize("shape", [4, 8, 10, 12, 13])
+def test_a_cap_far_above_the_scores_changes_nothing(shape, cap, fp32):
+    """cap tanh(z / cap) is z but for z^3 / (3 cap^2), below 1e-9 here."""
+    rows, lens, hq, hkv, hd = ATT_SHAPES[shape]
+    c = Case(rows, lens, hq, hkv, hd, torch.float32 if fp32 else torch.bfloat16, seed=shape)
+    q = (2 * randn(shape + 40, c.n_rows, hq * hd)).to(c.dtype)
+    want, tol = attention_reference(c, q)
+    got = sb.op_paged_attention(c.kv, q, hq, softcap=cap, layer=c.layer)
+    # quotient, square, three steps of the series that count, product: 8 roundings of z more, beside the hd + 4 of its bound
+    bad = ~((got.double() - want).abs() <= tol * (1 + 8 / (hd + 4)))
+    assert not bad.any(), (int(bad.sum()), float(((got.double() - want).abs() / tol).max()))
+
+
+@pytest.mark.parametrize("cap", [512.0, 513.0])
+@pytest.mark.parametrize("shape", [4, 12, 13])
+def test_both_ways_to_cap_the_scores(shape, cap):
+    rows, lens, hq, hkv, hd = ATT_SHAPES[shape]
+    c = Case(rows, lens, hq, hkv, hd, torch.bfloat16, seed=shape)
+    check_attention(c, (2 * randn(shape + 60, c.n_rows, hq * hd)).to(c.dtype), cap=cap, scale=4.0)
+
+
+@pytest.mark.parametrize("fp32", [True, False], ids=["fp32", "bf16"])
 @pytest.mark.parametrize("shape", [3, 5, 10, 11, 12, 13])
 def test_rows_that_see_nothing_get_zeros(shape, fp32):
     rows, lens, hq, hkv, hd = ATT_SHAPES[shape]
@@ -530,6 +553,23 @@ def test_row_starts_and_lengths_out_of_range_are_cut():
     c.row_start[:] = torch.tensor([5, 2, -3], dtype=torch.int32)   # descending: no rows
     out = torch.full((c.n_rows, 256), 7.0, device=DEV)
     assert (sb.op_paged_attention(c.kv, q, 4, out=out) == 7).all()
+
+
+@pytest.mark.parametrize("starts", [[100, 150, 0, 64], [200, 0, 210, 40], [7, 6, 300, 5]])
+def test_row_starts_that_do_not_ascend_stay_within_the_operands(starts):
+    """Which rows are worked on is open then; nothing else is touched, and the next call is as ever."""
+    c = Case([70, 60, 200], [5000, 3000, 4000], 6, 2, 64, torch.float32, seed=4)
+    q = randn(2, c.n_rows, 384)
+    want = sb.op_paged_attention(c.kv, q, 6)
+    scratch = sb.paged_attention_scratch(c.kv, 6)
+    assert scratch.numel() > 256          # (the keys are split)
+    scratch.fill_(0x7f)
+    good, pool, keep = c.row_start.clone(), c.pool.clone(), torch.full((3 * c.n_rows, 384), 7.0, device=DEV)
+    c.row_start.copy_(torch.tensor(starts, dtype=torch.int32))
+    sb.op_paged_attention(c.kv, q, 6, out=keep[c.n_rows:2 * c.n_rows], scratch=scratch)
+    assert (keep[:c.n_rows] == 7).all() and (keep[2 * c.n_rows:] == 7).all() and torch.equal(c.pool, pool)
+    c.row_start.copy_(good)
+    assert torch.equal(sb.op_paged_attention(c.kv, q, 6, scratch=scratch), want)
 
 
 def test_empty_batches():

@@ -72,6 +72,12 @@ def test_paged_attention_refusals(bad):
     assert attention(**bad) == sb.EINVAL
 
 
+@pytest.mark.parametrize("rule", [dict(softcap=2e30), dict(scale=1e30, softcap=1e-5), dict(scale=1e-20, softcap=1e15), dict(scale=2e38)], ids=str)
+def test_paged_attention_refuses_caps_that_floats_cannot_hold(rule):
+    """cap tanh(scale q.k / cap) needs scale / cap and log2(e) cap."""
+    assert attention(rule=B.sb_attn_rule(**rule)) == sb.EINVAL
+
+
 def test_paged_attention_scratch_refusals():
     kv = paged(max_len=16 * 4096, table_ld=4096)   # (long enough that the keys are split)
     n = sb.lib().sb_op_paged_attention_scratch_bytes(C.byref(kv), 32)
@@ -104,6 +110,24 @@ def copy(dst=P, dn=8, src=Q, sn=9, page=1024, slabs=4, to=(0, 1), frm=(3, 3), n=
     dict(src=P, sn=8, to=(4, 1), frm=(4, 2)), dict(to=tuple(range(8)) + (0,), frm=(1,) * 9)], ids=str)
 def test_copy_pages_refusals(bad):
     assert copy(**bad) == sb.EINVAL
+
+
+def test_copy_pages_refuses_pages_of_more_than_a_launch_counts():
+    assert copy(page=(1 << 27) + 16, dn=1, sn=1, slabs=1, src=P + (1 << 40), to=(0,), frm=(0,)) == sb.EINVAL
+
+
+def test_page_lists_that_32_bits_cannot_hold():
+    p = sb.Pages(4)
+    p.alloc(4)
+    for bad in ([1 << 32], np.array([(1 << 32) + 1]), np.array([-(1 << 40)])):
+        with pytest.raises(ValueError):
+            p.share(bad)
+    for bad in ([1.0], np.array([0.5])):
+        with pytest.raises(TypeError):
+            p.release(bad)
+    p.share(np.array([2, 3], dtype=np.int64))
+    p.share([])
+    assert [p.users(i) for i in range(4)] == [1, 1, 2, 2]
 
 
 def test_copy_of_no_pages_is_done():
