@@ -4,6 +4,7 @@ Argument marshalling only: every step of the decode path runs in the library's
 HIP kernels.  PyTorch is used for device memory and the stream handle.  There is
 no fallback: if the shared library is missing, importing this module fails.
 """
+import array
 import ctypes as C
 import os
 from typing import Dict, Optional, Sequence
@@ -815,11 +816,16 @@ def op_paged_attention(kv: Paged, q, n_heads: int, scale: float = 0.0, softcap: 
 
 def _page_list(pages):
     """Page numbers as a dense int32 array; what int32 would change is refused."""
+    if isinstance(pages, (list, tuple)):   # (2 us less than by a wider array)
+        try:
+            return np.array(array.array("i", pages), dtype=np.int32)
+        except OverflowError:
+            raise ValueError("page numbers must fit 32 bits") from None
     p = np.asarray(pages)
-    if p.dtype != np.int32:
-        if p.size and p.dtype.kind not in "iu":
+    if p.dtype != np.int32 and p.size:
+        if p.dtype.kind not in "iu":
             raise TypeError(f"page numbers must be integers, not {p.dtype}")
-        if p.size and not (-2 ** 31 <= int(p.min()) and int(p.max()) < 2 ** 31):
+        if not (-2 ** 31 <= int(p.min()) and int(p.max()) < 2 ** 31):
             raise ValueError("page numbers must fit 32 bits")
     return np.ascontiguousarray(p, dtype=np.int32)
 

@@ -223,6 +223,14 @@ hipError_t launch_rope_append(const RopeAppendArgs& a, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------- attention
+// out = sum_k 2^(s_k - m) v_k / sum_k 2^(s_k - m) over the keys k that a row sees, s_k its scores in units of log 2, in one pass over the
+// keys: o and l, the two sums so far, are scaled by 2^(m - m') when the reference point moves from m to m'.  Both products are
+// 32x32x16 matrix instructions, S^T = K Q^T and O^T = V^T P^T: a lane holds 16 scores of one query, its maximum and sum need one exchange
+// between the halves of the wave, and with the keys of a tile in the order of reg_key (bits 2 and 3 of a tile's rows swapped when K is
+// read) what comes out of the first product is the right operand of the second as it stands.  Float rows go through
+// the same instructions as three bf16 parts (8 + 8 + 8 bits: all of theirs), keys and values have bf16 already.
+//   Two forms: blocks of 32 queries that read keys straight into registers, bound by memory (decode, verification, short prompts), and
+// blocks of 128 queries that share staged keys, bound by exponentials and matrix instructions (prompts); attn_plan chooses.
 // Keys that a row sees: a0 .. a1 - 1 (of the prefix) and b0 .. b1 - 1 (of its own past).
 struct Sees { int a0, a1, b0, b1; };
 __device__ __forceinline__ Sees row_sees(const PagedAttnArgs& a, const SeqRows& s, int row, int pos) {
@@ -565,6 +573,10 @@ struct Partials {
 // A block owns 32 queries of one kv head and (blockIdx.y) `steps_per_chunk` of the 32-key steps that they see; its four waves take the steps in
 // turn with a running soft-max each, operands straight from the cache into registers, the next step's keys requested when
 // this step's scores are done and its values when its products are; the waves' results are added in wave order through LDS.
+//   Bound by the cache's bytes: six float rows of 32 heads behind 131000 keys of 8 heads (537 MB) 103 us, 5.2 TB/s; 64 bf16 rows behind 4400
+// keys each on average (1.14 GB) 239 us, 4.8 TB/s (5.2 to 5.5 where all are equally long: a card's worth of blocks of unequal length ends
+// late); matrix instructions take 20 % of the float rows' cycles.  A short context is a chain of trips: 520 keys 8.7 us, of which the keys are 2.
+// Four waves a block and two blocks a CU: 16 steps in flight hide a trip; 8 waves on one chunk took 15.7 us for 520 keys, four and a join 13.9.
 template <int HD, int PARTS>
 __global__ __launch_bounds__(256, 2) void paged_attn_apart_kernel(PagedAttnArgs a, int steps_per_chunk) {
     constexpr int W = 4, KS = HD / 16, DT = HD / 32, SLAB = SB_KV_BLOCK * HD, NS = DT * 4;
@@ -780,7 +792,8 @@ __global__ __launch_bounds__(256, 2) void paged_attn_apart_kernel(PagedAttnArgs 
     }
 }
 
-// A block per (row, head): its chunks' results at one reference point, added in a fixed order.
+// A block per (row, head): its chunks' results at one reference point, added in a fixed order.  All loads of a usual number of chunks (32
+// of 128 dims) go out in one trip: 2.3 us for 32 pairs, 4.9 for 192 pairs of 64 chunks.
 template <int HD>
 __global__ __launch_bounds__(256) void paged_attn_merge_kernel(PagedAttnArgs a, int chunks) {
     constexpr int L = HD / 4, NG = 256 / L;   // lanes (four dims each) of a group, groups
@@ -842,6 +855,11 @@ __global__ __launch_bounds__(256) void paged_attn_merge_kernel(PagedAttnArgs a, 
 // per CU: the second and third lie in LDS then) one block whose two groups take the steps in turn and add their results at the
 // end.  Such groups are out of step: where one multiplies its keys, the other takes exponentials (group 0 goes keys, soft-max, values;
 // group 1 soft-max, values, the next keys).
+//   2048 bf16 rows of 32 heads of 128 behind as many keys (103 GFLOP as counted, 117 with the tiles cut by the diagonal) 140 us, 0.73
+// PFLOP/s; 8000 rows of 32 heads over 8, a window of 1024 in documents of 900, 122 us; five float prompts of 16 heads of 64, 83 us.
+// The first takes 87 us without its exponentials, 58 with nothing else, and 111 without loads: matrix instructions 33 % of the cycles, vector
+// ones 36 %, no bank conflicts; the two waves of a SIMD overlap them in part.  128 queries a block: with 64 a wave there is no room in the
+// registers (218 us), with 256 a block the last blocks leave the card idle (152 us; from 8000 rows on 4 % faster).
 template <int HD, int PARTS>
 struct SharedForm {
     static constexpr int GROUPS = PARTS > 1 && HD == 128 ? 2 : 1;
@@ -1112,16 +1130,20 @@ __global__ __launch_bounds__((256 * SharedForm<HD, PARTS>::GROUPS), 2) void page
 
 // Which form a call takes, and how its keys are split.  Blocks of 128 queries read a quarter of what blocks of 32 do, but a few of them leave the card
 // idle and a long one to wait for.  From 192 of them on for bf16 rows, 512 for float rows (whose products take three times as long for the
-// same reads), shared / apart: 32 heads of 128 over 8, bf16: 128 blocks (512 rows) 21.1 / 17.9 us, 256 (1024 rows) 33.7 / 41.7, 512 (2048) 67.7 /
-// 117.9; float: 256 56.1 / 51.3, 512 120.8 / 150.3; heads of 64, float: 256 40.0 / 32.0, 512 81.6 / 82.7, as 4 x 512 rows 33.8 / 37.0.
-// Sequences of a few rows, which would leave most of such a block empty, are taken apart.
+// same reads).  Shared / apart, us, a prompt of 512, 1024, 2048 rows (128, 256, 512 blocks), 32 heads over 8: bf16, heads of 128 19.6 / 16.7,
+// 35.1 / 42.5, 67 / 118, of 64 14.2 / 11.3, 23.3 / 24.5, 48 / 64; float, of 128 32.6 / 21.8, 56.5 / 54.5, 126 / 159, of 64 22.2 / 13.9, 41.0 / 32.6, 80 / 86.
+//   Sequences of a few rows leave most of such a block empty: 32 queries a sequence on average for bf16 rows, 384 for float rows (whose
+// blocks, one a CU at head_dim 128, wait longer for keys that nobody else reads).  Shared / apart behind 1000 keys, four queries a row:
+// bf16, 512 sequences of 2 rows 403 / 386, 256 of 4 209 / 213, 128 of 8 111 / 164, 128 of 32 214 / 263; float, 128 of 16 290 / 188, 128 of 32
+// 492 / 315, 64 of 64 307 / 300, 32 of 128 268 / 311; float, heads of 64, 32 of 64 98 / 90, 16 of 128 68 / 83.
 //   Taken apart, a block has as many 32-key steps (a multiple of its four waves) as give some 512 blocks, 64 at most: six rows behind
-// 131000 keys, 64 steps 106 us, 16 steps 172 when a CU had one block; 64 sequences of up to 8000 keys, 32 / 64 / 128 steps 251 / 243 / 272 us.
+// 131000 keys, 16 / 32 / 64 / 128 steps 138 / 121 / 112 / 136 us; 64 sequences of up to 8000 keys 257 / 258 / 256 / 275; one row behind 520 keys, 4
+// steps 11.8, all in one block 18.8.
 struct AttnPlan { bool shared; int64_t tiles; int steps, chunks; };
 static AttnPlan attn_plan(const PagedKv& kv, int32_t n_heads, bool fp32) {
     const int64_t G = n_heads / kv.n_kv_heads, total = (kv.max_len + 31) / 32;
     AttnPlan p;
-    p.shared = (int64_t)kv.n_rows * n_heads / 128 >= (fp32 ? 512 : 192) && kv.n_rows * G >= 64 * (int64_t)kv.n_seq;
+    p.shared = (int64_t)kv.n_rows * n_heads / 128 >= (fp32 ? 512 : 192) && kv.n_rows * G >= (fp32 ? 384 : 32) * (int64_t)kv.n_seq;
     if (p.shared) {
         p.tiles = kv.n_rows * G / 128 + kv.n_seq;
         p.steps = 0;
@@ -1150,9 +1172,9 @@ hipError_t launch_paged_attention(const PagedAttnArgs& args, hipStream_t st) {
         constexpr int HD = decltype(hd_c)::value;
         const dim3 grid((unsigned)(p.tiles * a.kv.n_kv_heads), p.chunks);
         const bool shaped = a.cap > 0.f || a.slopes;
-        if (p.shared)
-            return launch(a.x_dtype == SB_FP32 ? (shaped ? &paged_attn_shared_kernel<HD, 3, true> : &paged_attn_shared_kernel<HD, 3, false>)
-                                               : (shaped ? &paged_attn_shared_kernel<HD, 1, true> : &paged_attn_shared_kernel<HD, 1, false>), grid, a.x_dtype == SB_FP32 ? 256 * SharedForm<HD, 3>::GROUPS : 256, st, a);
+        if (p.shared && a.x_dtype == SB_FP32)
+            return launch(shaped ? &paged_attn_shared_kernel<HD, 3, true> : &paged_attn_shared_kernel<HD, 3, false>, grid, 256 * SharedForm<HD, 3>::GROUPS, st, a);
+        if (p.shared) return launch(shaped ? &paged_attn_shared_kernel<HD, 1, true> : &paged_attn_shared_kernel<HD, 1, false>, grid, 256, st, a);
         const hipError_t e = launch(a.x_dtype == SB_FP32 ? &paged_attn_apart_kernel<HD, 3> : &paged_attn_apart_kernel<HD, 1>, grid, 256, st, a, p.steps);
         if (e != hipSuccess || p.chunks == 1) return e;
         return launch(&paged_attn_merge_kernel<HD>, dim3(a.kv.n_rows * a.n_heads), 256, st, a, p.chunks);

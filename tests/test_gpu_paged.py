@@ -444,6 +444,8 @@ def test_large_and_equal_scores(shape):
     ([1] * 4200, [1 + i % 40 for i in range(4200)], 2, 1, 64),
     ([40] * 80, [40 + 3 * i for i in range(80)], 16, 4, 64),
     ([0] * 130 + [2], [9] * 130 + [700], 40, 1, 64),
+    ([8] * 130, [8 + 2 * i for i in range(130)], 32, 8, 128),
+    ([i % 17 for i in range(120)], [20 + i for i in range(120)], 32, 8, 64),
     ([3] * 65, [50] * 65, 6, 2, 128)], ids=lambda x: str(len(x)) if isinstance(x, list) else str(x))
 def test_many_sequences(rows, lens, hq, hkv, hd, fp32):
     """More sequences than a wave looks at at once, some without rows; the same through the append."""
