@@ -271,6 +271,45 @@ __device__ __forceinline__ SeqRows tile_seq(const PagedAttnArgs& a, int t, int& 
     return s;
 }
 
+// Sum over the wave, a scalar.
+template <int O = 32>
+__device__ __forceinline__ int wave_total(int v) {
+    uint32_t x, y;
+    lane_pair<O>((uint32_t)v, x, y);
+    if constexpr (O > 1) return wave_total<O / 2>((int)(x + y));
+    else return __builtin_amdgcn_readfirstlane((int)(x + y));
+}
+// The p-th longest tile of TQ queries among 64 sequences at most, a lane each: a tile's length is its sequence's past, in tiles, and its number there,
+// so sequence b has tiles of lengths B_b .. B_b + c_b - 1; x is the largest length that more than p tiles reach.
+template <int TQ>
+__device__ __forceinline__ SeqRows tile_by_length(const PagedAttnArgs& a, int p, int& q0) {
+    const int lane = threadIdx.x & 63, b = lane < a.kv.n_seq ? lane : 0;
+    const int r0 = row_at(a.kv, b), r1 = row_at(a.kv, b + 1), len = clampi(a.kv.kv_len[b], 0, a.kv.max_len);
+    const int n = lane < a.kv.n_seq && r1 > r0 ? r1 - r0 : 0, c = (n * a.group + TQ - 1) / TQ;
+    const int64_t past = (int64_t)(len > n ? len - n : 0) * a.group / TQ;
+    const int B = past < (1 << 28) ? (int)past : 1 << 28;
+    const auto reach = [&](int x) { return wave_total(clampi(B + c - x, 0, c)); };
+    SeqRows s{-1, 0, 0, 0};
+    q0 = 0;
+    if (p >= wave_total(c)) return s;
+    int lo = half_min<32>(c ? B : 0x7fffffff), hi = -half_min<32>(c ? -(B + c) : 0);   // reach(lo) > p >= reach(hi)
+    while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2;
+        if (reach(mid) > p) lo = mid;
+        else hi = mid;
+    }
+    const int nth = p - reach(lo + 1);   // among the sequences that have a tile of this length
+    const uint64_t have = __builtin_amdgcn_ballot_w64(B <= lo && lo < B + c);
+    const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(have >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)have, 0));
+    const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(B <= lo && lo < B + c && before == nth));
+    s.b = l;
+    s.r0 = __builtin_amdgcn_readlane(r0, l);
+    s.n = __builtin_amdgcn_readlane(n, l);
+    s.len = __builtin_amdgcn_readlane(len, l);
+    q0 = (lo - __builtin_amdgcn_readlane(B, l)) * TQ;
+    return s;
+}
+
 // Row of query qq of a sequence (heads of one kv head's group per row).
 __device__ __forceinline__ int row_of(const PagedAttnArgs& a, int qq) { return a.group_shift >= 0 ? qq >> a.group_shift : qq / a.group; }
 
@@ -887,10 +926,20 @@ __global__ __launch_bounds__((256 * SharedForm<HD, PARTS>::GROUPS), 2) void page
     const int Hkv = a.kv.n_kv_heads, tiles = gridDim.x / Hkv;
     const int g = blockIdx.x % Hkv;
     int q0;
-    const SeqRows s = tile_seq<BQ>(a, tiles - 1 - (int)(blockIdx.x / Hkv), q0);   // (a prompt's last rows see most: they start first)
+    const int p = blockIdx.x / Hkv;   // (a prompt's last rows see most: they start first)
+    const SeqRows s = a.kv.n_seq > 1 && a.kv.n_seq <= 64 ? tile_by_length<BQ>(a, p, q0) : tile_seq<BQ>(a, tiles - 1 - p, q0);
     if (s.b < 0) return;
     Reach w;
     const Query q = lane_query(a, s, g, q0 + wave * 32, li, w);
+    // The queries go out now, their trip runs beside the search for the steps and the first pages.
+    using Raw = std::conditional_t<PARTS == 1, bf16x8, float4>;
+    constexpr int RAW = PARTS == 1 ? 1 : 2;
+    Raw raw[KS][RAW];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int x = 0; x < RAW; ++x)
+            raw[ks][x] = reinterpret_cast<const Raw*>(reinterpret_cast<const char*>(a.q) + ((int64_t)q.row * a.ld_q + q.head * HD + lh * 8 + ks * 16) * (2 * RAW))[x];
     if (lane == 0 && grp == 0) {
         int* const r = reach_s[wave];
         r[0] = w.a_lo; r[1] = w.b_lo; r[2] = w.a1_min; r[3] = w.b1_min;
@@ -948,7 +997,8 @@ __global__ __launch_bounds__((256 * SharedForm<HD, PARTS>::GROUPS), 2) void page
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         bf16x8 t[PARTS];
-        load8_split<PARTS>(a.q, (int64_t)q.row * a.ld_q + q.head * HD + lh * 8 + ks * 16, t);
+        if constexpr (PARTS == 1) t[0] = raw[ks][0];
+        else split8<PARTS>(raw[ks][0], raw[ks][1], t);
 #pragma unroll
         for (int x = 0; x < PARTS; ++x)
             if (x < PARTS - IN_LDS) qo[x][ks] = t[x];
@@ -1090,12 +1140,27 @@ __global__ __launch_bounds__((256 * SharedForm<HD, PARTS>::GROUPS), 2) void page
     const float l_own = lanes_sum<32, 32>(l_run);
     if constexpr (GROUPS == 1) {
         const float inv_l = l_own == 0.f ? 0.f : 1.0f / l_own;
-        if (!q.valid) return;
+        // Rows leave whole: a wave turns its own in LDS (piece p of row r at p ^ r % 16), so that a store covers whole lines.
+        constexpr int P = HD * (PARTS == 1 ? 2 : 4) / 16, RPI = 64 / P;   // 16-byte pieces of a row, rows of a store
+        char* const t_s = reinterpret_cast<char*>(&kv_s[0][0][0][0]) + wave * 32 * P * 16;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4)
-                store_out4<HD>(a, q, dt * 32 + 2 * r + 4 * lh, make_float4(o[dt][r] * inv_l, o[dt][r + 1] * inv_l, o[dt][r + 2] * inv_l, o[dt][r + 3] * inv_l));
+            for (int r = 0; r < 16; r += 4) {
+                const float4 v = make_float4(o[dt][r] * inv_l, o[dt][r + 1] * inv_l, o[dt][r + 2] * inv_l, o[dt][r + 3] * inv_l);
+                if constexpr (PARTS == 1) *reinterpret_cast<uint2*>(t_s + (li * P + ((dt * 4 + r / 4) ^ (li & (P - 1)))) * 16 + lh * 8) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+                else *reinterpret_cast<float4*>(t_s + (li * P + ((dt * 8 + r / 2 + lh) ^ (li & (P - 1)))) * 16) = v;
+            }
+        const int nq = s.n * a.group - (q0 + wave * 32);   // queries of this wave from here on
+#pragma unroll
+        for (int i = 0; i < 32 / RPI; ++i) {
+            const int x = i * RPI + lane / P, p = lane % P;
+            const uint4 v = *reinterpret_cast<const uint4*>(t_s + (x * P + (p ^ (x & (P - 1)))) * 16);
+            if (x >= nq) continue;
+            const int qq = q0 + wave * 32 + x, r = row_of(a, qq);
+            char* const to = reinterpret_cast<char*>(a.out) + ((int64_t)(s.r0 + r) * a.ld_out + (g * a.group + qq - r * a.group) * HD) * (PARTS == 1 ? 2 : 4);
+            *reinterpret_cast<uint4*>(to + p * 16) = v;
+        }
         return;
     }
     // ---- the groups' results at one reference point: each keeps half of the dims and gives the other half away
