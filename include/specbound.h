@@ -490,7 +490,7 @@ int32_t sb_op_rope_append(const sb_paged *kv, int32_t layer, const void *qkv, in
  * All zeros: plain causal attention. */
 typedef struct sb_attn_rule {
     float scale;               /* 0: 1 / sqrt(head_dim); else > 0 */
-    float softcap;             /* 0: none; else > 0 (1e30 at most, scale / softcap in 1e-34 .. 1e34) */
+    float softcap;             /* 0: none; else > 0 (1e30 at most, scale / softcap in 1e-34 .. 1e6) */
     const float *slopes;       /* NULL, or device [n_heads] */
     int32_t window;            /* 0: none; else the row's own key counts: window 1 sees that alone */
     const int32_t *prefix_len; /* NULL, or device [n_seq]: so many first keys are seen by every row (kv_len: all) */

@@ -416,19 +416,25 @@ __device__ __forceinline__ void load8_split(const void* rows, int64_t at, bf16x8
 // Register r of a key tile's scores in lane (li, lh): query li, key key0 + 16 (r / 8) + 8 lh + r % 8.
 __device__ __forceinline__ int reg_key(int r) { return (r >> 3) * 16 + (r & 7); }
 
-// tanh x to a few units in the last place: below 0.3 its series up to x^11 (the next term is 2e-9 of x there), else 1 - 2 / (exp 2x + 1).
-__device__ __forceinline__ float tanh_low(float x) {
-    const float y = x * x;
-    float t = fmaf(y, -8.8632355e-3f, 2.1869488e-2f);
-    t = fmaf(y, t, -5.3968254e-2f);
-    t = fmaf(y, t, 0.13333333f);
-    t = fmaf(y, t, -0.33333333f);
-    return fmaf(x * y, t, x);
-}
-__device__ __forceinline__ float tanh_near(float x) {
-    const float e = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(fabsf(x) * (2.f * LOG2E)) + 1.f), 1.f);
-    return fabsf(x) < 0.3f ? tanh_low(x) : copysignf(e, x);
-}
+// A capped score c2 tanh(s k), in units of log 2, to a few units in the last place.  Where |s k| < 0.3 it is z (1 + y (a1 + y (a2 + y a3))), y = (s k)^2, z = c2 k s: the
+// polynomial of this form nearest to tanh x / x there (1.3e-8 of it), its coefficients times powers of k^2, so that s k itself is not needed; else
+// 1 - 2 / (exp(2 |s k|) + 1).  A score's bits do not depend on the scores beside it.
+struct Cap {
+    float k, c2, z, b1, b2, b3;
+    __device__ __forceinline__ Cap(float k_, float c2_) : k(k_), c2(c2_), z(k_ * c2_) {
+        const float kk = k * k;
+        b1 = -0.33333060f * kk; b2 = 0.13314833f * (kk * kk); b3 = -0.050366241f * (kk * kk * kk);
+    }
+    __device__ __forceinline__ float low(float s) const {
+        const float y = s * s, w = s * z;
+        return fmaf(w * y, fmaf(y, fmaf(y, b3, b2), b1), w);
+    }
+    __device__ __forceinline__ float any(float s) const {
+        const float x = fabsf(s) * k;
+        const float e = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * LOG2E)) + 1.f), 1.f);
+        return x < 0.3f ? low(s) : copysignf(c2 * e, s);
+    }
+};
 // Cap and bias, where there are any: scores in units of log 2 then, raw products else.
 template <int PARTS, int KT, bool SHAPED>
 __device__ __forceinline__ void shape_scores(const PagedAttnArgs& a, const Query& q, int key0, int lh, f32x16 (&st)[KT]) {
@@ -442,21 +448,24 @@ __device__ __forceinline__ void shape_scores(const PagedAttnArgs& a, const Query
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     st[t][r] = fmaf(-2.f * c2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(st[t][r] * k) + 1.f), c2);
-        } else {   // (mostly all scores of a tile are far below the cap, where the series alone does)
-            const float k = a.scale / a.cap;
+        } else {   // (mostly all scores of a tile are far below the cap, where the polynomial alone does)
+            const Cap cap(a.scale / a.cap, c2);
             float top = 0.f;
 #pragma unroll
             for (int t = 0; t < KT; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    st[t][r] *= k;
-                    top = __builtin_elementwise_maximum(top, fabsf(st[t][r]));
-                }
-            const bool low = __builtin_amdgcn_ballot_w64(!(top < 0.3f)) == 0;
+                for (int r = 0; r < 16; ++r) top = __builtin_elementwise_maximum(top, fabsf(st[t][r]));
+            if (__builtin_amdgcn_ballot_w64(!(top * cap.k < 0.3f)) == 0) {
 #pragma unroll
-            for (int t = 0; t < KT; ++t)
+                for (int t = 0; t < KT; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) st[t][r] = c2 * (low ? tanh_low(st[t][r]) : tanh_near(st[t][r]));
+                    for (int r = 0; r < 16; ++r) st[t][r] = cap.low(st[t][r]);
+            } else {
+#pragma unroll
+                for (int t = 0; t < KT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) st[t][r] = cap.any(st[t][r]);
+            }
         }
     } else if (a.slopes) {
         const float c2 = a.scale * LOG2E;

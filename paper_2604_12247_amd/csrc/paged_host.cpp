@@ -114,7 +114,7 @@ int32_t sb_op_paged_attention(const sb_paged* kv, int32_t layer, const void* q, 
     if (!(r.scale >= 0.f) || r.scale > 1e38f) return fail(SB_EINVAL, "%s: scale must be positive, or 0 for 1 / sqrt(head_dim)", op);
     const float scale = r.scale > 0.f ? r.scale : 1.0f / sqrtf((float)kv->head_dim);
     if (!(r.softcap >= 0.f) || r.softcap > 1e30f) return fail(SB_EINVAL, "%s: softcap must be positive and 1e30 at most, or 0 for none", op);
-    if (r.softcap > 0.f && !(scale / r.softcap >= 1e-34f && scale / r.softcap <= 1e34f)) return fail(SB_EINVAL, "%s: scale / softcap must be in 1e-34..1e34", op);
+    if (r.softcap > 0.f && !(scale / r.softcap >= 1e-34f && scale / r.softcap <= 1e6f)) return fail(SB_EINVAL, "%s: scale / softcap must be in 1e-34..1e6", op);
     if (r.window < 0) return fail(SB_EINVAL, "%s: window must be positive, or 0 for none", op);
     if (empty) return SB_OK;
     if (((uintptr_t)r.slopes | (uintptr_t)r.prefix_len | (uintptr_t)r.doc_start) & 3) return fail(SB_EINVAL, "%s: misaligned slopes, prefix_len or doc_start", op);

@@ -72,7 +72,7 @@ def test_paged_attention_refusals(bad):
     assert attention(**bad) == sb.EINVAL
 
 
-@pytest.mark.parametrize("rule", [dict(softcap=2e30), dict(scale=1e30, softcap=1e-5), dict(scale=1e-20, softcap=1e15), dict(scale=2e38)], ids=str)
+@pytest.mark.parametrize("rule", [dict(softcap=2e30), dict(scale=4.0, softcap=1e-6), dict(scale=1e-20, softcap=1e15), dict(scale=2e38)], ids=str)
 def test_paged_attention_refuses_caps_that_floats_cannot_hold(rule):
     """cap tanh(scale q.k / cap) needs scale / cap and log2(e) cap."""
     assert attention(rule=B.sb_attn_rule(**rule)) == sb.EINVAL
