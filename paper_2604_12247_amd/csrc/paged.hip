@@ -280,7 +280,8 @@ __device__ __forceinline__ int wave_total(int v) {
     else return __builtin_amdgcn_readfirstlane((int)(x + y));
 }
 // The p-th longest tile of TQ queries among 64 sequences at most, a lane each: a tile's length is its sequence's past, in tiles, and its number there,
-// so sequence b has tiles of lengths B_b .. B_b + c_b - 1; x is the largest length that more than p tiles reach.
+// so sequence b has tiles of lengths B_b .. B_b + c_b - 1; `lo` ends as the largest length that more than p tiles reach.  (Some 500 blocks run at once:
+// with the sequences one behind the other, the longest two on one CU, five capped float prompts took 89 us, so 82; five of 100 to 2000 bf16 rows 62, so 56.)
 template <int TQ>
 __device__ __forceinline__ SeqRows tile_by_length(const PagedAttnArgs& a, int p, int& q0) {
     const int lane = threadIdx.x & 63, b = lane < a.kv.n_seq ? lane : 0;
@@ -402,17 +403,6 @@ __device__ __forceinline__ void split8(float4 x, float4 y, bf16x8 (&op)[PARTS]) 
         op[i] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
     }
 }
-// Eight values of a row as operands: bf16 rows as they are, float rows in three parts.
-template <int PARTS>
-__device__ __forceinline__ void load8_split(const void* rows, int64_t at, bf16x8 (&op)[PARTS]) {
-    if constexpr (PARTS == 1) {
-        op[0] = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const uint16_t*>(rows) + at);
-    } else {
-        const float* p = reinterpret_cast<const float*>(rows) + at;
-        split8<PARTS>(*reinterpret_cast<const float4*>(p), *reinterpret_cast<const float4*>(p + 4), op);
-    }
-}
-
 // Register r of a key tile's scores in lane (li, lh): query li, key key0 + 16 (r / 8) + 8 lh + r % 8.
 __device__ __forceinline__ int reg_key(int r) { return (r >> 3) * 16 + (r & 7); }
 
@@ -903,11 +893,12 @@ __global__ __launch_bounds__(256) void paged_attn_merge_kernel(PagedAttnArgs a, 
 // per CU: the second and third lie in LDS then) one block whose two groups take the steps in turn and add their results at the
 // end.  Such groups are out of step: where one multiplies its keys, the other takes exponentials (group 0 goes keys, soft-max, values;
 // group 1 soft-max, values, the next keys).
-//   2048 bf16 rows of 32 heads of 128 behind as many keys (103 GFLOP as counted, 117 with the tiles cut by the diagonal) 140 us, 0.73
-// PFLOP/s; 8000 rows of 32 heads over 8, a window of 1024 in documents of 900, 122 us; five float prompts of 16 heads of 64, 83 us.
-// The first takes 87 us without its exponentials, 58 with nothing else, and 111 without loads: matrix instructions 33 % of the cycles, vector
-// ones 36 %, no bank conflicts; the two waves of a SIMD overlap them in part.  128 queries a block: with 64 a wave there is no room in the
-// registers (218 us), with 256 a block the last blocks leave the card idle (152 us; from 8000 rows on 4 % faster).
+//   2048 bf16 rows of 32 heads of 128 behind as many keys (103 GFLOP as counted, 105 with the steps cut by the diagonal) 138 us, 0.75
+// PFLOP/s; 8000 rows of 32 heads over 8, a window of 1024 in documents of 900, 116 us; five float prompts of 16 heads of 64, capped, 59 us.
+// The first takes 87 us without its exponentials, 58 with those alone, and 111 without loads: matrix instructions 34 % of the cycles, vector
+// ones 38 %, no bank conflicts; the two waves of a SIMD overlap them in part, and the clock falls (with zeros for operands 126 where it takes 156).
+// 128 queries a block: with 64 a wave there is no room in the registers (218 us), with 256 a block the last blocks leave the card
+// idle (152 us; from 8000 rows on 4 % faster).
 template <int HD, int PARTS>
 struct SharedForm {
     static constexpr int GROUPS = PARTS > 1 && HD == 128 ? 2 : 1;
@@ -944,11 +935,12 @@ __global__ __launch_bounds__((256 * SharedForm<HD, PARTS>::GROUPS), 2) void page
     using Raw = std::conditional_t<PARTS == 1, bf16x8, float4>;
     constexpr int RAW = PARTS == 1 ? 1 : 2;
     Raw raw[KS][RAW];
+    const int64_t q_at = ((int64_t)q.row * a.ld_q + q.head * HD + lh * 8) * (2 * RAW);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
         for (int x = 0; x < RAW; ++x)
-            raw[ks][x] = reinterpret_cast<const Raw*>(reinterpret_cast<const char*>(a.q) + ((int64_t)q.row * a.ld_q + q.head * HD + lh * 8 + ks * 16) * (2 * RAW))[x];
+            raw[ks][x] = reinterpret_cast<const Raw*>(reinterpret_cast<const char*>(a.q) + q_at + ks * 32 * RAW)[x];
     if (lane == 0 && grp == 0) {
         int* const r = reach_s[wave];
         r[0] = w.a_lo; r[1] = w.b_lo; r[2] = w.a1_min; r[3] = w.b1_min;
@@ -1204,12 +1196,12 @@ __global__ __launch_bounds__((256 * SharedForm<HD, PARTS>::GROUPS), 2) void page
 
 // Which form a call takes, and how its keys are split.  Blocks of 128 queries read a quarter of what blocks of 32 do, but a few of them leave the card
 // idle and a long one to wait for.  From 192 of them on for bf16 rows, 512 for float rows (whose products take three times as long for the
-// same reads).  Shared / apart, us, a prompt of 512, 1024, 2048 rows (128, 256, 512 blocks), 32 heads over 8: bf16, heads of 128 19.6 / 16.7,
-// 35.1 / 42.5, 67 / 118, of 64 14.2 / 11.3, 23.3 / 24.5, 48 / 64; float, of 128 32.6 / 21.8, 56.5 / 54.5, 126 / 159, of 64 22.2 / 13.9, 41.0 / 32.6, 80 / 86.
-//   Sequences of a few rows leave most of such a block empty: 32 queries a sequence on average for bf16 rows, 384 for float rows (whose
+// same reads).  Shared / apart, us, a prompt of 512, 1024, 2048 rows (128, 256, 512 blocks), 32 heads over 8: bf16, heads of 128 18.6 / 16.8,
+// 34.4 / 42.5, 65 / 118, of 64 13.5 / 11.3, 22.6 / 24.6, 48 / 65; float, of 128 32.8 / 21.7, 56.2 / 53.7, 121 / 152, of 64 21.6 / 13.4, 40.2 / 31.6, 79 / 83.
+//   Sequences of a few rows leave most of such a block empty: 32 queries a sequence on average for bf16 rows, 192 for float rows (whose
 // blocks, one a CU at head_dim 128, wait longer for keys that nobody else reads).  Shared / apart behind 1000 keys, four queries a row:
-// bf16, 512 sequences of 2 rows 403 / 386, 256 of 4 209 / 213, 128 of 8 111 / 164, 128 of 32 214 / 263; float, 128 of 16 290 / 188, 128 of 32
-// 492 / 315, 64 of 64 307 / 300, 32 of 128 268 / 311; float, heads of 64, 32 of 64 98 / 90, 16 of 128 68 / 83.
+// bf16, 512 sequences of 2 rows 397 / 383, 256 of 4 206 / 212, 128 of 8 111 / 164, 128 of 32 205 / 263; float, 128 of 16 281 / 186, 128 of 32
+// 487 / 306, 64 of 64 282 / 294, 32 of 128 261 / 290; float, heads of 64, 32 of 64 64 / 80, 16 of 128 63 / 75.
 //   Taken apart, a block has as many 32-key steps (a multiple of its four waves) as give some 512 blocks, 64 at most: six rows behind
 // 131000 keys, 16 / 32 / 64 / 128 steps 138 / 121 / 112 / 136 us; 64 sequences of up to 8000 keys 257 / 258 / 256 / 275; one row behind 520 keys, 4
 // steps 11.8, all in one block 18.8.
@@ -1217,7 +1209,7 @@ struct AttnPlan { bool shared; int64_t tiles; int steps, chunks; };
 static AttnPlan attn_plan(const PagedKv& kv, int32_t n_heads, bool fp32) {
     const int64_t G = n_heads / kv.n_kv_heads, total = (kv.max_len + 31) / 32;
     AttnPlan p;
-    p.shared = (int64_t)kv.n_rows * n_heads / 128 >= (fp32 ? 512 : 192) && kv.n_rows * G >= (fp32 ? 384 : 32) * (int64_t)kv.n_seq;
+    p.shared = (int64_t)kv.n_rows * n_heads / 128 >= (fp32 ? 512 : 192) && kv.n_rows * G >= (fp32 ? 192 : 32) * (int64_t)kv.n_seq;
     if (p.shared) {
         p.tiles = kv.n_rows * G / 128 + kv.n_seq;
         p.steps = 0;

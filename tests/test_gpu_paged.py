@@ -446,9 +446,11 @@ def test_large_and_equal_scores(shape):
     ([0] * 130 + [2], [9] * 130 + [700], 40, 1, 64),
     ([8] * 130, [8 + 2 * i for i in range(130)], 32, 8, 128),
     ([i % 17 for i in range(120)], [20 + i for i in range(120)], 32, 8, 64),
+    ([(13 * i) % 60 for i in range(40)], [(13 * i) % 60 + 100 * (i % 3) for i in range(40)], 64, 8, 64),
+    ([300, 0, 300, 1, 299], [300, 0, 300, 4000, 600], 64, 8, 128),
     ([3] * 65, [50] * 65, 6, 2, 128)], ids=lambda x: str(len(x)) if isinstance(x, list) else str(x))
 def test_many_sequences(rows, lens, hq, hkv, hd, fp32):
-    """More sequences than a wave looks at at once, some without rows; the same through the append."""
+    """Sequences without rows or equally long ones, more of them than a wave looks at at once; the same through the append."""
     dt = torch.float32 if fp32 else torch.bfloat16
     c = Case(rows, lens, hq, hkv, hd, dt, seed=len(rows), lead=1, tail=2, junk=math.nan)
     cos, sin = (torch.from_numpy(t).to(DEV) for t in sb.rope_table_scaled(hd, 10000.0, max(lens)))
