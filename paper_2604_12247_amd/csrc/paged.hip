@@ -279,36 +279,74 @@ __device__ __forceinline__ int wave_total(int v) {
     if constexpr (O > 1) return wave_total<O / 2>((int)(x + y));
     else return __builtin_amdgcn_readfirstlane((int)(x + y));
 }
-// The p-th longest tile of TQ queries among 64 sequences at most, a lane each: a tile's length is its sequence's past, in tiles, and its number there,
-// so sequence b has tiles of lengths B_b .. B_b + c_b - 1; `lo` ends as the largest length that more than p tiles reach.  (Some 500 blocks run at once:
-// with the sequences one behind the other, the longest two on one CU, five capped float prompts took 89 us, so 82; five of 100 to 2000 bf16 rows 62, so 56.)
-template <int TQ>
+// The p-th longest tile of TQ queries among 64 R sequences at most, R a lane: a tile's length is its sequence's past, in tiles, and its number there,
+// so sequence b has tiles of lengths B_b .. B_b + c_b - 1; `lo` ends as the largest length that more than p tiles reach.
+template <int TQ, int R>
 __device__ __forceinline__ SeqRows tile_by_length(const PagedAttnArgs& a, int p, int& q0) {
-    const int lane = threadIdx.x & 63, b = lane < a.kv.n_seq ? lane : 0;
-    const int r0 = row_at(a.kv, b), r1 = row_at(a.kv, b + 1), len = clampi(a.kv.kv_len[b], 0, a.kv.max_len);
-    const int n = lane < a.kv.n_seq && r1 > r0 ? r1 - r0 : 0, c = (n * a.group + TQ - 1) / TQ;
-    const int64_t past = (int64_t)(len > n ? len - n : 0) * a.group / TQ;
-    const int B = past < (1 << 28) ? (int)past : 1 << 28;
-    const auto reach = [&](int x) { return wave_total(clampi(B + c - x, 0, c)); };
+    const int lane = threadIdx.x & 63;
+    int r0[R], n[R], len[R], c[R], B[R];
+    int all = 0, least = 0x7fffffff, most = 0;
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+        const int b = 64 * u + lane < a.kv.n_seq ? 64 * u + lane : 0;
+        const int r1 = row_at(a.kv, b + 1);
+        r0[u] = row_at(a.kv, b);
+        len[u] = clampi(a.kv.kv_len[b], 0, a.kv.max_len);
+        n[u] = 64 * u + lane < a.kv.n_seq && r1 > r0[u] ? r1 - r0[u] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+        c[u] = (n[u] * a.group + TQ - 1) / TQ;
+        const int64_t past = (int64_t)(len[u] > n[u] ? len[u] - n[u] : 0) * a.group / TQ;
+        B[u] = past < (1 << 28) ? (int)past : 1 << 28;
+        all += c[u];
+        if (c[u] && B[u] < least) least = B[u];
+        if (c[u] && B[u] + c[u] > most) most = B[u] + c[u];
+    }
+    const auto reach = [&](int x) {
+        int v = 0;
+#pragma unroll
+        for (int u = 0; u < R; ++u) v += clampi(B[u] + c[u] - x, 0, c[u]);
+        return wave_total(v);
+    };
     SeqRows s{-1, 0, 0, 0};
     q0 = 0;
-    if (p >= wave_total(c)) return s;
-    int lo = half_min<32>(c ? B : 0x7fffffff), hi = -half_min<32>(c ? -(B + c) : 0);   // reach(lo) > p >= reach(hi)
+    if (p >= wave_total(all)) return s;
+    int lo = half_min<32>(least), hi = -half_min<32>(-most);   // reach(lo) > p >= reach(hi)
     while (hi - lo > 1) {
         const int mid = lo + (hi - lo) / 2;
         if (reach(mid) > p) lo = mid;
         else hi = mid;
     }
-    const int nth = p - reach(lo + 1);   // among the sequences that have a tile of this length
-    const uint64_t have = __builtin_amdgcn_ballot_w64(B <= lo && lo < B + c);
-    const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(have >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)have, 0));
-    const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(B <= lo && lo < B + c && before == nth));
-    s.b = l;
-    s.r0 = __builtin_amdgcn_readlane(r0, l);
-    s.n = __builtin_amdgcn_readlane(n, l);
-    s.len = __builtin_amdgcn_readlane(len, l);
-    q0 = (lo - __builtin_amdgcn_readlane(B, l)) * TQ;
+    int nth = p - reach(lo + 1);   // among the sequences that have a tile of this length
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+        const bool has = B[u] <= lo && lo < B[u] + c[u];
+        const uint64_t have = __builtin_amdgcn_ballot_w64(has);
+        const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(have >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)have, 0));
+        const uint64_t it = __builtin_amdgcn_ballot_w64(has && before == nth);
+        nth -= __popcll(have);
+        if (it == 0) continue;
+        const int l = __builtin_ctzll(it);
+        s.b = 64 * u + l;
+        s.r0 = __builtin_amdgcn_readlane(r0[u], l);
+        s.n = __builtin_amdgcn_readlane(n[u], l);
+        s.len = __builtin_amdgcn_readlane(len[u], l);
+        q0 = (lo - __builtin_amdgcn_readlane(B[u], l)) * TQ;
+    }
     return s;
+}
+// Tile t of a call: longest first where there are LEAST sequences or more (256 at most: every block sorts them, 0.6 to 1.2 us) that may be long, else as they
+// lie.  As they lie / longest first, us: one row each of 64 sequences of up to 8000 keys 255 / 240, 3000 108 / 92, 500 21.7 / 20.4, 200 13.6 / 14.1, of 16 of up
+// to 3000 40.7 / 41.8, of 128 of up to 3000 191 / 176, 100 17.9 / 19.7; five capped float prompts 89 / 82, five of 100 to 2000 bf16 rows 62 / 56; 10 to 100 rows
+// of 80 sequences behind up to 1500 139 / 116, up to 200 rows of 100 with no past 71 / 78.
+template <int TQ, int LEAST, bool LAST_FIRST>
+__device__ __forceinline__ SeqRows tile_of(const PagedAttnArgs& a, int t, int tiles, int& q0) {
+    if (a.kv.n_seq >= LEAST && a.kv.max_len >= 512) {
+        if (a.kv.n_seq <= 64) return tile_by_length<TQ, 1>(a, t, q0);
+        if (a.kv.n_seq <= 256) return tile_by_length<TQ, 4>(a, t, q0);
+    }
+    return tile_seq<TQ>(a, LAST_FIRST ? tiles - 1 - t : t, q0);
 }
 
 // Row of query qq of a sequence (heads of one kv head's group per row).
@@ -612,9 +650,9 @@ struct Partials {
 // turn with a running soft-max each, operands straight from the cache into registers, the next step's keys requested when
 // this step's scores are done and its values when its products are; the waves' results are added in wave order through LDS.
 //   Bound by the cache's bytes: six float rows of 32 heads behind 131000 keys of 8 heads (537 MB) 103 us, 5.2 TB/s; 64 bf16 rows behind 4400
-// keys each on average (1.14 GB) 239 us, 4.8 TB/s (5.2 to 5.5 where all are equally long: a card's worth of blocks of unequal length ends
-// late); matrix instructions take 20 % of the float rows' cycles.  A short context is a chain of trips: 520 keys 8.7 us, of which the keys are 2.
-// Four waves a block and two blocks a CU: 16 steps in flight hide a trip; 8 waves on one chunk took 15.7 us for 520 keys, four and a join 13.9.
+// keys each on average (1.14 GB) 226 us, 5.0 TB/s (5.2 to 5.5 where all are equally long: the last blocks end apart); matrix instructions
+// take 20 % of the float rows' cycles.  A short context is a chain of trips: 520 keys 9 to 10 us, of which the keys are 2.
+// Four waves a block and two blocks a CU: eight steps in flight hide a trip; 8 waves on one chunk took 15.7 us for 520 keys, four and a join 13.9.
 template <int HD, int PARTS>
 __global__ __launch_bounds__(256, 2) void paged_attn_apart_kernel(PagedAttnArgs a, int steps_per_chunk) {
     constexpr int W = 4, KS = HD / 16, DT = HD / 32, SLAB = SB_KV_BLOCK * HD, NS = DT * 4;
@@ -624,7 +662,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_apart_kernel(PagedAttnArgs 
     const int li = lane & 31, lh = lane >> 5;
     const int Hkv = a.kv.n_kv_heads, g = blockIdx.x % Hkv;
     int q0;
-    const SeqRows s = tile_seq<32>(a, blockIdx.x / Hkv, q0);
+    const SeqRows s = tile_of<32, 32, false>(a, blockIdx.x / Hkv, gridDim.x / Hkv, q0);
     if (s.b < 0) return;
     Reach w;
     const Query q = lane_query(a, s, g, q0, li, w);
@@ -926,8 +964,7 @@ __global__ __launch_bounds__((256 * SharedForm<HD, PARTS>::GROUPS), 2) void page
     const int Hkv = a.kv.n_kv_heads, tiles = gridDim.x / Hkv;
     const int g = blockIdx.x % Hkv;
     int q0;
-    const int p = blockIdx.x / Hkv;   // (a prompt's last rows see most: they start first)
-    const SeqRows s = a.kv.n_seq > 1 && a.kv.n_seq <= 64 ? tile_by_length<BQ>(a, p, q0) : tile_seq<BQ>(a, tiles - 1 - p, q0);
+    const SeqRows s = tile_of<BQ, 2, true>(a, blockIdx.x / Hkv, tiles, q0);   // (a prompt's last rows see most: they start first)
     if (s.b < 0) return;
     Reach w;
     const Query q = lane_query(a, s, g, q0 + wave * 32, li, w);
@@ -1149,7 +1186,9 @@ __global__ __launch_bounds__((256 * SharedForm<HD, PARTS>::GROUPS), 2) void page
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const float4 v = make_float4(o[dt][r] * inv_l, o[dt][r + 1] * inv_l, o[dt][r + 2] * inv_l, o[dt][r + 3] * inv_l);
-                if constexpr (PARTS == 1) *reinterpret_cast<uint2*>(t_s + (li * P + ((dt * 4 + r / 4) ^ (li & (P - 1)))) * 16 + lh * 8) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+                if constexpr (PARTS == 1)
+                    *reinterpret_cast<uint2*>(t_s + (li * P + ((dt * 4 + r / 4) ^ (li & (P - 1)))) * 16 + lh * 8) =
+                        make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
                 else *reinterpret_cast<float4*>(t_s + (li * P + ((dt * 8 + r / 2 + lh) ^ (li & (P - 1)))) * 16) = v;
             }
         const int nq = s.n * a.group - (q0 + wave * 32);   // queries of this wave from here on

@@ -448,6 +448,9 @@ def test_large_and_equal_scores(shape):
     ([i % 17 for i in range(120)], [20 + i for i in range(120)], 32, 8, 64),
     ([(13 * i) % 60 for i in range(40)], [(13 * i) % 60 + 100 * (i % 3) for i in range(40)], 64, 8, 64),
     ([300, 0, 300, 1, 299], [300, 0, 300, 4000, 600], 64, 8, 128),
+    ([i % 3 for i in range(200)], [i % 3 + (37 * i) % 900 for i in range(200)], 8, 2, 64),
+    ([1 + i % 16 for i in range(256)], [16 + 3 * i for i in range(256)], 16, 4, 128),
+    ([1] * 40, [1 + 50 * (i % 20) for i in range(40)], 8, 2, 128),
     ([3] * 65, [50] * 65, 6, 2, 128)], ids=lambda x: str(len(x)) if isinstance(x, list) else str(x))
 def test_many_sequences(rows, lens, hq, hkv, hd, fp32):
     """Sequences without rows or equally long ones, more of them than a wave looks at at once; the same through the append."""
