@@ -477,7 +477,15 @@ __device__ __forceinline__ void shape_scores(const PagedAttnArgs& a, const Query
                 for (int r = 0; r < 16; ++r)
                     st[t][r] = fmaf(-2.f * c2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(st[t][r] * k) + 1.f), c2);
         } else {   // (mostly all scores of a tile are far below the cap, where the polynomial alone does)
-            const Cap cap(a.scale / a.cap, c2);
+            float k = a.scale / a.cap;
+            if (k < 1e-3f) {   // (k^6 and the squares of such scores leave float's range)
+#pragma unroll
+                for (int t = 0; t < KT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) st[t][r] *= k;
+                k = 1.f;
+            }
+            const Cap cap(k, c2);
             float top = 0.f;
 #pragma unroll
             for (int t = 0; t < KT; ++t)

@@ -357,6 +357,18 @@ def test_a_cap_far_above_the_scores_changes_nothing(shape, cap, fp32):
     assert not bad.any(), (int(bad.sum()), float(((got.double() - want).abs() / tol).max()))
 
 
+@pytest.mark.parametrize("fp32", [True, False], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("shape", [4, 12, 13])
+def test_a_cap_above_scores_whose_squares_floats_cannot_hold(shape, fp32):
+    """Scores of 1e20 far below a cap of 1e30: one key has all the weight, as without a cap."""
+    rows, lens, hq, hkv, hd = ATT_SHAPES[shape]
+    c = Case(rows, lens, hq, hkv, hd, torch.float32 if fp32 else torch.bfloat16, seed=shape + 3)
+    q = (1e20 * randn(shape + 80, c.n_rows, hq * hd)).to(c.dtype)
+    want = sb.op_paged_attention(c.kv, q, hq, scale=1.0, layer=c.layer)
+    got = sb.op_paged_attention(c.kv, q, hq, scale=1.0, softcap=1e30, layer=c.layer)
+    assert torch.isfinite(want.float()).all() and torch.equal(got, want)
+
+
 @pytest.mark.parametrize("cap", [512.0, 513.0])
 @pytest.mark.parametrize("shape", [4, 12, 13])
 def test_both_ways_to_cap_the_scores(shape, cap):
