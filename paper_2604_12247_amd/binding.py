@@ -794,6 +794,10 @@ def op_paged_attention(kv: Paged, q, n_heads: int, scale: float = 0.0, softcap: 
     code = _dtype_code(q)
     rule = None
     if scale or softcap or window or slopes is not None or prefix_len is not None or doc_start is not None:
+        for v, name in ((scale, "scale"), (softcap, "softcap")):
+            if v and abs(v) < 1e-37:
+                raise ValueError(f"{name} must be 0 or a float of 32 bits, not {v}")
+        window = max(-1, min(window, 0x7fffffff))   # (no sequence is that long)
         rule = C.byref(sb_attn_rule(scale, softcap, _vector(slopes, "slopes", n_heads, torch.float32, index), window,
                                     _vector(prefix_len, "prefix_len", kv.n_seq, torch.int32, index),
                                     _vector(doc_start, "doc_start", kv.n_rows, torch.int32, index)))

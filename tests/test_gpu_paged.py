@@ -694,6 +694,13 @@ def test_binding_refusals():
         rope(rope_cos=cos[:, :6].contiguous(), rope_sin=sin[:, :6].contiguous())
     with pytest.raises(sb.SbError):
         att(softcap=-1.0)
+    for bad in (dict(window=-1), dict(window=-(1 << 32) + 5)):
+        with pytest.raises(sb.SbError):
+            att(**bad)
+    for bad in (dict(scale=1e-50), dict(softcap=1e-60)):   # (0 in 32 bits: another rule)
+        with pytest.raises(ValueError):
+            att(**bad)
+    assert torch.equal(att(window=(1 << 32) + 1), att())
     with pytest.raises(sb.SbError):
         rope(out=qkv[:, 8:264])
     mk = lambda **k: sb.Paged(**{**dict(pool=c.pool, table=c.table, row_start=c.row_start, kv_len=c.kv_len, n_rows=2), **k})
