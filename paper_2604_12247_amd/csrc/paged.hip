@@ -939,8 +939,8 @@ __global__ __launch_bounds__(256) void paged_attn_merge_kernel(PagedAttnArgs a, 
 // per CU: the second and third lie in LDS then) one block whose two groups take the steps in turn and add their results at the
 // end.  Such groups are out of step: where one multiplies its keys, the other takes exponentials (group 0 goes keys, soft-max, values;
 // group 1 soft-max, values, the next keys).
-//   2048 bf16 rows of 32 heads of 128 behind as many keys (103 GFLOP as counted, 105 with the steps cut by the diagonal) 138 us, 0.75
-// PFLOP/s; 8000 rows of 32 heads over 8, a window of 1024 in documents of 900, 116 us; five float prompts of 16 heads of 64, capped, 59 us.
+//   2048 bf16 rows of 32 heads of 128 behind as many keys (103 GFLOP as counted, 105 with the steps cut by the diagonal) 136 us, 0.76
+// PFLOP/s; 8000 rows of 32 heads over 8, a window of 1024 in documents of 900, 116 us; five float prompts of 16 heads of 64, capped, 60 us.
 // The first takes 87 us without its exponentials, 58 with those alone, and 111 without loads: matrix instructions 34 % of the cycles, vector
 // ones 38 %, no bank conflicts; the two waves of a SIMD overlap them in part, and the clock falls (with zeros for operands 126 where it takes 156).
 // 128 queries a block: with 64 a wave there is no room in the registers (218 us), with 256 a block the last blocks leave the card
